@@ -175,7 +175,7 @@ def prepare(case, seed):
         total[order[b]] = rows[b] + ctx[b]
     if own:
         from paper_2605_08862_amd.runtime import KvqCache
-        cache = KvqCache(1, Hq, Hkv, D, n, max(total), B_max=n, q_max=max(rows), device=DEVICE, page_perm_seed=seed, slot_tokens=total)
+        cache = KvqCache(1, Hq, Hkv, D, n, max(total), q_max=max(rows), device=DEVICE, page_perm_seed=seed, slot_tokens=total)
     else:
         pages = [(t + PAGE - 1) // PAGE for t in total]
         ids = torch.randperm(sum(pages), generator=torch.Generator().manual_seed(seed)).to(torch.int32)
