@@ -263,6 +263,82 @@ bs_status bs_kv_write(bs_ctx* ctx, int layer, int slot, int pos0, int n, const v
 bs_status bs_kv_read(bs_ctx* ctx, int layer, int slot, int pos0, int n, void* k_rows, void* v_rows,
                      void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * KV cache in 8 bits.  Half of the bytes of the 16-bit cache, for rollouts whose contexts bound the batch or the step.
+ *
+ * A block is one page (BS_PAGE_TOKENS tokens) of one KV head; K and V have blocks of their own.  A block holds OCP e4m3 codes and
+ * one scale, value = code * scale.  Scales are powers of two 2^e with e in [-15, 7]: the least one with which every row that was
+ * written fits, max|x| <= 448 * 2^e.  A write that begins a block (row 0 of its page is among the rows) sets the scale; a write
+ * behind rows that are there keeps the larger of the old scale and its own, and rounds the older rows of the block again if the
+ * scale grew (exact but for elements below 2^-6 of the new scale).  Rounding is to nearest, ties to even.  |x| > 57344 is
+ * saturated to +-57344 and NaN to 0, with BS_FAULT_RANGE.  Every value held is exact in float16 and in bfloat16.
+ *
+ * These calls need no context.  The caller owns all memory.  They only enqueue work on `stream` (of the current device), can be
+ * captured into a HIP graph, and report conditions only the device can see in `status` (dev, one int32 word that the caller
+ * clears; BS_FAULT_* bits are or-ed into it; may be NULL).  Rows are packed in batch order: sequence b has n[b] rows, which start
+ * at sum_{b'<b} n[b'] (a count outside [0, n_max] sets BS_FAULT_DRAFT_LEN and counts as 0).  A sequence with a bad slot
+ * (BS_FAULT_SLOT), or with positions or page ids outside the cache (BS_FAULT_KV_PAGES), is skipped: its rows of the outputs and
+ * its pages stay as they are.  A sequence without rows is skipped whatever its slot is (padded batches). */
+typedef struct {
+  int32_t n_pages, n_slots, max_pages_per_seq, n_kv_heads, head_dim;
+  void* k_pages;              /* dev [n_pages] pages of n_kv_heads * BS_PAGE_TOKENS * head_dim bytes, 16-byte aligned; element  */
+  void* v_pages;              /* order private to the library; zero-fill once (masked positions enter products with weight 0)  */
+  float* k_scale;             /* dev [n_pages, n_kv_heads]                                                                     */
+  float* v_scale;             /* dev [n_pages, n_kv_heads]                                                                     */
+  const int32_t* block_table; /* dev [n_slots, max_pages_per_seq], as in bs_kv_desc                                            */
+} bs_kvq_desc;
+
+/* Writes rows [n, n_kv_heads, head_dim] bf16 (row_stride elements from one row to the next, at least n_kv_heads * head_dim) to
+ * positions pos0[b] .. pos0[b] + n_rows[b] of slot seq_slot[b], n_rows[b] <= n_max.  Positions before pos0 must have been written,
+ * positions behind the last row become undefined.  Of sequences with the same slot only the first is written (BS_FAULT_SLOT).
+ * Errors: BS_EINVAL (null, misaligned pages), BS_ESHAPE (head_dim not in {64, 128}, n_kv_heads outside [1, 256], B outside
+ * [1, 4096], n_max outside [1, max_pages_per_seq * BS_PAGE_TOKENS], row_stride too small, a launch of more than 2^23 pages), BS_EHIP. */
+bs_status bs_kvq_write(const bs_kvq_desc* kv, int B, const int32_t* seq_slot /*[B]*/, const int32_t* pos0 /*[B]*/,
+                       const int32_t* n_rows /*[B]*/, int n_max, const void* k_rows, const void* v_rows, int64_t row_stride,
+                       int32_t* status, void* stream);
+/* The reverse: the values held, as bf16 (exact).  Slots may repeat.  Same errors. */
+bs_status bs_kvq_read(const bs_kvq_desc* kv, int B, const int32_t* seq_slot, const int32_t* pos0, const int32_t* n_rows, int n_max,
+                      void* k_rows, void* v_rows, int64_t row_stride, int32_t* status, void* stream);
+
+/* Ragged causal attention over the cache.  Sequence b has q_len[b] <= q_max packed query rows [n_q_heads, head_dim] (bf16,
+ * q_stride elements from one row to the next, at least n_q_heads * head_dim) at positions ctx_len[b] .. ctx_len[b] + q_len[b];
+ * their own K/V rows have been written before.  Row i sees positions 0 .. ctx_len[b] + i:
+ *   out = softmax(q K^T / sqrt(head_dim)) V,   out: bf16 [rows, n_q_heads, head_dim], packed.
+ * Query head j reads KV head j / (n_q_heads / n_kv_heads).  Products run on float16 operands (queries beyond +-65504 are
+ * saturated, NaN becomes 0, BS_FAULT_RANGE) with float32 accumulation and softmax.
+ * workspace (dev, 256-byte aligned, at least bs_kvq_workspace_bytes of the same n_q_heads, n_kv_heads, head_dim and of a q_max no
+ * smaller) is zero-filled once before its first use; calls that share one must not overlap in time.
+ * Errors: BS_EINVAL (null, q or out not on 16 bytes, q_stride not a multiple of 8, misaligned workspace), BS_ESHAPE (as above;
+ * n_q_heads not a multiple of n_kv_heads or more than 128 to one, q_max outside [1, max_pages_per_seq * BS_PAGE_TOKENS]),
+ * BS_ECAPACITY (workspace too small), BS_EHIP. */
+size_t bs_kvq_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim, int q_max);   /* 0 on invalid arguments */
+bs_status bs_kvq_attention(const bs_kvq_desc* kv, int B, const int32_t* seq_slot /*[B]*/, const int32_t* ctx_len /*[B]*/,
+                           const int32_t* q_len /*[B]*/, int q_max, int n_q_heads, const void* q, int64_t q_stride, void* out,
+                           int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Log probabilities of a rollout's tokens under the distribution that made them (what importance weights need when rollouts come
+ * from a quantised cache or an older policy), the entropy of that distribution and its best alternatives.
+ * logits [M, vocab] (dev, logits_dtype, dense) are packed as in bs_accept_resample_logits: sequence b has draft_len[b] + 1 rows
+ * (draft_len == NULL: k_max + 1 each); token i < n_tokens[b] <= draft_len[b] + 1 (NULL: all rows) of sequence b is tokens[b][i], judged by row i.
+ * So the outputs of an accept call can be passed on: tokens = out_tokens, n_tokens = n_emitted.  Over p = softmax(logits / temperature):
+ *   logprob[b][i] = log p(token);   entropy[b][i] = -sum p log p (may be NULL);
+ *   top_tokens / top_logprobs [b][i][0..n_top): the n_top largest logits, equal ones by the lower token first.
+ * Masked tokens (-inf) have log p = -inf and are no alternatives; places without one hold -1 and -inf.  A row in which everything
+ * is masked: logprob -inf, entropy 0.  A row with NaN or +inf: NaN (alternatives: what is not NaN, by logit).
+ * Entries i >= n_tokens[b] and tokens outside [0, vocab) (BS_FAULT_TOKEN_ID) hold 0, 0, -1, 0; so does a sequence whose draft_len or
+ * n_tokens is out of range (BS_FAULT_DRAFT_LEN; a draft_len outside [0, k_max] counts no rows).  status: as above.
+ * workspace (dev, 256-byte aligned, at least bs_token_logprobs_workspace_bytes of the same vocab and n_top and of B and k_max no smaller) is zero-filled
+ * once before its first use; calls that share one must not overlap in time.
+ * Errors: BS_EINVAL (null, temperature or its reciprocal not in (0, inf), bad dtype, logits not aligned to their elements), BS_ESHAPE (vocab < 2 or > 2^24, n_top outside
+ * [0, 32] or above vocab, B or k_max + 1 outside [1, 4096], more than 2^20 rows), BS_ECAPACITY (workspace too small), BS_EHIP. */
+size_t bs_token_logprobs_workspace_bytes(int B, int k_max, int vocab, int n_top);   /* 0 on invalid arguments */
+bs_status bs_token_logprobs(int B, int vocab, const void* logits, int logits_dtype, const int32_t* draft_len /*[B] or NULL*/,
+                            int k_max, const int32_t* tokens /*[B,k_max+1]*/, const int32_t* n_tokens /*[B] or NULL*/,
+                            float temperature, int n_top, float* logprob /*[B,k_max+1]*/, float* entropy /*[B,k_max+1] or NULL*/,
+                            int32_t* top_tokens /*[B,k_max+1,n_top]*/, float* top_logprobs /*[B,k_max+1,n_top]*/,
+                            int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Measurement hooks (not part of Alg. 1): time every launch of one kernel class of the following
  * bs_verify_step / bs_accept_resample calls with HIP events recorded on the call's own stream.
  * bs_profile_begin selects the class (BS_PROF_*) and clears the counters; bs_profile_end synchronises

@@ -19,7 +19,8 @@ STATUS_NAMES = ["BS_OK", "BS_EINVAL", "BS_ESHAPE", "BS_ECAPACITY", "BS_ESTATE", 
 EXPORTS = ["bs_workspace_bytes", "bs_create", "bs_destroy", "bs_last_error", "bs_pool_bind", "bs_draft_lookup",
            "bs_verify_step", "bs_accept_resample", "bs_accept_resample_logits", "bs_kv_commit", "bs_kv_write",
            "bs_kv_read", "bs_poll_status", "bs_profile_begin", "bs_profile_end", "bs_index_build", "bs_index_free",
-           "bs_index_bind", "bs_set_filter", "bs_kv_lengths", "bs_accept_resample_logits_noalloc"]
+           "bs_index_bind", "bs_set_filter", "bs_kv_lengths", "bs_accept_resample_logits_noalloc", "bs_kvq_write", "bs_kvq_read",
+           "bs_kvq_workspace_bytes", "bs_kvq_attention", "bs_token_logprobs_workspace_bytes", "bs_token_logprobs"]
 PROF_CLASSES = {"attention": 1, "gemm_qkv": 2, "gemm_o": 3, "gemm_gate_up": 4, "gemm_down": 5, "lmhead": 6,
                 "sample": 7, "lookup": 8, "empty": 9}
 
@@ -41,6 +42,12 @@ class bs_kv_desc(C.Structure):
     _fields_ = [("n_pages", C.c_int32), ("n_slots", C.c_int32), ("max_pages_per_seq", C.c_int32),
                 ("k_pages", C.POINTER(C.c_void_p)), ("v_pages", C.POINTER(C.c_void_p)),
                 ("block_table", C.c_void_p), ("ctx_len", C.c_void_p)]
+
+
+class bs_kvq_desc(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("n_slots", C.c_int32), ("max_pages_per_seq", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("block_table", C.c_void_p)]
 
 
 _lib = None
@@ -83,8 +90,16 @@ def lib():
         L.bs_poll_status.argtypes = [vp, vp, C.POINTER(C.c_int32)]
         L.bs_profile_begin.argtypes = [vp, i32]
         L.bs_profile_end.argtypes = [vp, vp, C.POINTER(C.c_float), C.POINTER(C.c_int)]
+        L.bs_kvq_write.argtypes = [vp, i32, vp, vp, vp, i32, vp, vp, C.c_int64, vp, vp]
+        L.bs_kvq_read.argtypes = L.bs_kvq_write.argtypes
+        L.bs_kvq_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.bs_kvq_workspace_bytes.restype = C.c_size_t
+        L.bs_kvq_attention.argtypes = [vp, i32, vp, vp, vp, i32, i32, vp, C.c_int64, vp, vp, vp, C.c_size_t, vp]
+        L.bs_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.bs_token_logprobs_workspace_bytes.restype = C.c_size_t
+        L.bs_token_logprobs.argtypes = [i32, i32, vp, i32, vp, i32, vp, vp, f32, i32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
         for name in EXPORTS:
-            if name not in ("bs_workspace_bytes", "bs_destroy", "bs_last_error", "bs_index_free"):
+            if name not in ("bs_kvq_workspace_bytes", "bs_token_logprobs_workspace_bytes", "bs_workspace_bytes", "bs_destroy", "bs_last_error", "bs_index_free"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -246,6 +261,84 @@ def bs_kv_write(ctx, layer, slot, pos0, n, k_rows, v_rows):
 
 def bs_kv_read(ctx, layer, slot, pos0, n, k_rows, v_rows):
     _check(ctx, lib().bs_kv_read(ctx, layer, slot, pos0, n, _ptr(k_rows), _ptr(v_rows), _stream()))
+
+
+def _on_current_device(*tensors):
+    """The calls without a context launch on the current device's stream: a tensor of another device is refused."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise BsError(BS_EINVAL, "tensor on %s, current device cuda:%d" % (t.device, dev))
+
+
+def _rows(t, width):
+    """(address, elements from one row to the next) of packed rows [n, ..., ...] whose inner dimensions are dense."""
+    inner = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size != 1 and stride != inner:
+            raise BsError(BS_EINVAL, "the inner dimensions of the rows must be dense")
+        inner *= size
+    if inner != width:
+        raise BsError(BS_ESHAPE, "rows of %d elements, %d expected" % (inner, width))
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else width)
+
+
+def make_kvq_desc(kv):
+    """kv: dict(n_pages, n_slots, max_pages_per_seq, n_kv_heads, head_dim, and the tensors k_pages, v_pages (uint8), k_scale,
+    v_scale (float32), block_table).  The description holds addresses only: the caller keeps the tensors."""
+    return bs_kvq_desc(kv["n_pages"], kv["n_slots"], kv["max_pages_per_seq"], kv["n_kv_heads"], kv["head_dim"], kv["k_pages"].data_ptr(),
+                       kv["v_pages"].data_ptr(), kv["k_scale"].data_ptr(), kv["v_scale"].data_ptr(), kv["block_table"].data_ptr())
+
+
+def _kvq_copy(name, desc, B, seq_slot, pos0, n_rows, n_max, k_rows, v_rows, status):
+    _on_current_device(seq_slot, pos0, n_rows, k_rows, v_rows, status)
+    width = desc.n_kv_heads * desc.head_dim
+    if k_rows.dtype != torch.bfloat16 or v_rows.dtype != torch.bfloat16:
+        raise BsError(BS_EINVAL, name + ": rows are bfloat16")
+    (k, ks), (v, vs) = _rows(k_rows, width), _rows(v_rows, width)
+    if ks != vs:
+        raise BsError(BS_EINVAL, name + ": K and V rows must have the same stride")
+    st = getattr(lib(), name)(C.byref(desc), B, _ptr(seq_slot), _ptr(pos0), _ptr(n_rows), n_max, k, v, ks, _ptr(status), _stream())
+    if st != BS_OK:
+        raise BsError(st, name)
+
+
+def bs_kvq_write(desc, B, seq_slot, pos0, n_rows, n_max, k_rows, v_rows, status=None):
+    _kvq_copy("bs_kvq_write", desc, B, seq_slot, pos0, n_rows, n_max, k_rows, v_rows, status)
+
+
+def bs_kvq_read(desc, B, seq_slot, pos0, n_rows, n_max, k_rows, v_rows, status=None):
+    _kvq_copy("bs_kvq_read", desc, B, seq_slot, pos0, n_rows, n_max, k_rows, v_rows, status)
+
+
+def bs_kvq_workspace_bytes(n_q_heads, n_kv_heads, head_dim, q_max):
+    return lib().bs_kvq_workspace_bytes(n_q_heads, n_kv_heads, head_dim, q_max)
+
+
+def bs_kvq_attention(desc, B, seq_slot, ctx_len, q_len, q_max, n_q_heads, q, out, workspace, status=None):
+    _on_current_device(seq_slot, ctx_len, q_len, q, out, workspace, status)
+    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
+        raise BsError(BS_EINVAL, "bs_kvq_attention: q and out are bfloat16")
+    address, stride = _rows(q, n_q_heads * desc.head_dim)
+    st = lib().bs_kvq_attention(C.byref(desc), B, _ptr(seq_slot), _ptr(ctx_len), _ptr(q_len), q_max, n_q_heads, address, stride, _ptr(out), _ptr(status),
+                                _ptr(workspace), workspace.numel() * workspace.element_size(), _stream())
+    if st != BS_OK:
+        raise BsError(st, "bs_kvq_attention")
+
+
+def bs_token_logprobs_workspace_bytes(B, k_max, vocab, n_top):
+    return lib().bs_token_logprobs_workspace_bytes(B, k_max, vocab, n_top)
+
+
+def bs_token_logprobs(B, vocab, logits, draft_len, k_max, tokens, n_tokens, temperature, n_top, logprob, entropy, top_tokens, top_logprobs,
+                      workspace, status=None):
+    _on_current_device(logits, draft_len, tokens, n_tokens, logprob, entropy, top_tokens, top_logprobs, workspace, status)
+    dtype = {torch.float32: BS_F32, torch.bfloat16: BS_BF16}.get(logits.dtype, -1)
+    st = lib().bs_token_logprobs(B, vocab, _ptr(logits), dtype, _ptr(draft_len), k_max, _ptr(tokens), _ptr(n_tokens), temperature, n_top, _ptr(logprob),
+                                 _ptr(entropy), _ptr(top_tokens), _ptr(top_logprobs), _ptr(status), _ptr(workspace),
+                                 workspace.numel() * workspace.element_size(), _stream())
+    if st != BS_OK:
+        raise BsError(st, "bs_token_logprobs")
 
 
 def bs_poll_status(ctx):

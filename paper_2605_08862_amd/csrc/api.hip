@@ -1,6 +1,8 @@
 // C ABI of libbubblespec: argument validation, workspace carving and kernel sequencing of one
 // speculative-verification step (Alg. 1 of the paper; see include/bubblespec.h for the contract).
 #include "common.h"
+#include "kvq.h"
+#include "logprob.h"
 #include <mutex>
 #include <new>
 #include <string>
@@ -724,6 +726,85 @@ bs_status bs_accept_resample_logits_noalloc(int B, int vocab, const float* logit
   launch_clear_status(c->plan.status, (hipStream_t)stream);
   return accept_common(c, B, vocab, logits, draft_tokens, draft_len, k_max, q_logits, q_dtype, temperature, eos_id,
                        emit_bonus, u_accept, u_sample, n_accepted, out_tokens, n_emitted, near_tie, (hipStream_t)stream);
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// The 8-bit cache and the log probabilities: calls without a context.
+namespace {
+bs_status check_kvq(const bs_kvq_desc* d) {
+  if (!d || !d->k_pages || !d->v_pages || !d->k_scale || !d->v_scale || !d->block_table) return BS_EINVAL;
+  if ((((uintptr_t)d->k_pages | (uintptr_t)d->v_pages) & 15) || (((uintptr_t)d->k_scale | (uintptr_t)d->v_scale | (uintptr_t)d->block_table) & 3)) return BS_EINVAL;
+  if (d->n_pages < 1 || d->n_slots < 1 || d->max_pages_per_seq < 1 || d->max_pages_per_seq > (1 << 24)) return BS_ESHAPE;
+  if (d->n_kv_heads < 1 || d->n_kv_heads > 256 || (d->head_dim != 64 && d->head_dim != 128)) return BS_ESHAPE;
+  return BS_OK;
+}
+KvqView view_of(const bs_kvq_desc& d) {
+  return KvqView{d.n_pages, d.n_slots, d.max_pages_per_seq, d.n_kv_heads, d.head_dim, d.block_table, (uint8_t*)d.k_pages, (uint8_t*)d.v_pages, d.k_scale, d.v_scale};
+}
+bs_status last_hip() { return hipGetLastError() == hipSuccess ? BS_OK : BS_EHIP; }
+
+bs_status kvq_copy(const bs_kvq_desc* kv, int B, const int32_t* seq_slot, const int32_t* pos0, const int32_t* n_rows, int n_max, void* k_rows, void* v_rows,
+                   int64_t row_stride, int32_t* status, bool write, void* stream) {
+  const bs_status st = check_kvq(kv);
+  if (st != BS_OK) return st;
+  if (!seq_slot || !pos0 || !n_rows || !k_rows || !v_rows || (((uintptr_t)k_rows | (uintptr_t)v_rows) & 1)) return BS_EINVAL;
+  if (B < 1 || B > 4096 || n_max < 1 || (int64_t)n_max > (int64_t)kv->max_pages_per_seq * kPage) return BS_ESHAPE;
+  if (row_stride < (int64_t)kv->n_kv_heads * kv->head_dim || (int64_t)B * (n_max / kPage + 2) > (1 << 23)) return BS_ESHAPE;
+  const KvqSeqs q{B, n_max, 0, seq_slot, pos0, n_rows, nullptr, 0, 0};
+  if (write) launch_kvq_write(view_of(*kv), q, k_rows, v_rows, (size_t)row_stride, status, (hipStream_t)stream);
+  else launch_kvq_read(view_of(*kv), q, k_rows, v_rows, (size_t)row_stride, status, (hipStream_t)stream);
+  return last_hip();
+}
+bool kvq_heads_ok(int Hq, int Hkv, int D) {
+  return Hkv >= 1 && Hkv <= 256 && Hq >= Hkv && Hq % Hkv == 0 && Hq / Hkv <= 128 && (D == 64 || D == 128);
+}
+}  // namespace
+
+bs_status bs_kvq_write(const bs_kvq_desc* kv, int B, const int32_t* seq_slot, const int32_t* pos0, const int32_t* n_rows, int n_max, const void* k_rows,
+                       const void* v_rows, int64_t row_stride, int32_t* status, void* stream) {
+  return kvq_copy(kv, B, seq_slot, pos0, n_rows, n_max, (void*)k_rows, (void*)v_rows, row_stride, status, true, stream);
+}
+bs_status bs_kvq_read(const bs_kvq_desc* kv, int B, const int32_t* seq_slot, const int32_t* pos0, const int32_t* n_rows, int n_max, void* k_rows,
+                      void* v_rows, int64_t row_stride, int32_t* status, void* stream) {
+  return kvq_copy(kv, B, seq_slot, pos0, n_rows, n_max, k_rows, v_rows, row_stride, status, false, stream);
+}
+
+size_t bs_kvq_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim, int q_max) {
+  if (!kvq_heads_ok(n_q_heads, n_kv_heads, head_dim) || q_max < 1) return 0;
+  return kvq_attention_workspace(n_q_heads, n_kv_heads, head_dim, q_max);
+}
+bs_status bs_kvq_attention(const bs_kvq_desc* kv, int B, const int32_t* seq_slot, const int32_t* ctx_len, const int32_t* q_len, int q_max, int n_q_heads,
+                           const void* q, int64_t q_stride, void* out, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
+  const bs_status st = check_kvq(kv);
+  if (st != BS_OK) return st;
+  if (!seq_slot || !ctx_len || !q_len || !q || !out || !workspace) return BS_EINVAL;
+  if ((((uintptr_t)q | (uintptr_t)out) & 15) || q_stride % 8 || ((uintptr_t)workspace & 255)) return BS_EINVAL;
+  if (!kvq_heads_ok(n_q_heads, kv->n_kv_heads, kv->head_dim) || B < 1 || B > 4096 || q_max < 1 || (int64_t)q_max > (int64_t)kv->max_pages_per_seq * kPage ||
+      q_stride < (int64_t)n_q_heads * kv->head_dim)
+    return BS_ESHAPE;
+  if (workspace_bytes < kvq_attention_workspace(n_q_heads, kv->n_kv_heads, kv->head_dim, q_max)) return BS_ECAPACITY;
+  const KvqSeqs s{B, q_max, 0, seq_slot, ctx_len, q_len, nullptr, 0, 0};
+  launch_kvq_attention(view_of(*kv), s, n_q_heads, q, (size_t)q_stride, out, status, workspace, (hipStream_t)stream);
+  return last_hip();
+}
+
+size_t bs_token_logprobs_workspace_bytes(int B, int k_max, int vocab, int n_top) {
+  if (B < 1 || B > 4096 || k_max < 0 || k_max > 4095 || B * (k_max + 1) > (1 << 20) || vocab < 2 || vocab > (1 << 24) || n_top < 0 || n_top > kLogprobMaxTop || n_top > vocab)
+    return 0;
+  return logprob_workspace(B, k_max, vocab, n_top);
+}
+bs_status bs_token_logprobs(int B, int vocab, const void* logits, int logits_dtype, const int32_t* draft_len, int k_max, const int32_t* tokens,
+                            const int32_t* n_tokens, float temperature, int n_top, float* logprob, float* entropy, int32_t* top_tokens,
+                            float* top_logprobs, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!logits || !tokens || !logprob || !workspace || (n_top > 0 && (!top_tokens || !top_logprobs))) return BS_EINVAL;
+  if (logits_dtype != BS_F32 && logits_dtype != BS_BF16) return BS_EINVAL;
+  if (!(temperature > 0.f) || !(1.0f / temperature > 0.f) || !(1.0f / temperature <= 3.4028235e38f) || ((uintptr_t)logits & (logits_dtype == BS_F32 ? 3 : 1)) || ((uintptr_t)workspace & 255)) return BS_EINVAL;
+  const size_t need = bs_token_logprobs_workspace_bytes(B, k_max, vocab, n_top);
+  if (need == 0) return BS_ESHAPE;
+  if (workspace_bytes < need) return BS_ECAPACITY;
+  const LogprobArgs a{logits, draft_len, tokens, n_tokens, k_max, vocab, n_top, 1.0f / temperature, logprob, entropy, top_logprobs, top_tokens, status};
+  launch_logprob(a, B, logits_dtype, workspace, (hipStream_t)stream);
+  return last_hip();
 }
 
 // Not part of the public ABI: selects the unfused QKV path (projection GEMM, then the rotary / append kernel)

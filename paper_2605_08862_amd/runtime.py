@@ -25,6 +25,26 @@ def fuse_weights(w, dtype, device):
     return out
 
 
+def page_table(n_slots, max_ctx, slot_tokens, page_perm_seed, device):
+    """(block table [n_slots, most pages of a slot], number of pages): every slot gets the pages of max_ctx tokens, or of its own
+    entry of slot_tokens (entries beyond a slot's pages are -1); page_perm_seed scatters the page ids."""
+    P = B.BS_PAGE_TOKENS
+    caps = [int(max_ctx)] * n_slots if slot_tokens is None else [int(t) for t in slot_tokens]
+    assert len(caps) == n_slots
+    pages_of = [(c + P - 1) // P for c in caps]
+    n_pages = sum(pages_of)
+    ids = torch.arange(n_pages, dtype=torch.int32)
+    if page_perm_seed is not None:
+        g = torch.Generator().manual_seed(page_perm_seed)
+        ids = ids[torch.randperm(n_pages, generator=g)]
+    table = torch.full((n_slots, max(pages_of)), -1, dtype=torch.int32)
+    at = 0
+    for b, n in enumerate(pages_of):
+        table[b, :n] = ids[at:at + n]
+        at += n
+    return table.contiguous().to(device), n_pages
+
+
 class Engine:
     """Owns the device buffers of one context and forwards to the C ABI."""
 
@@ -41,28 +61,15 @@ class Engine:
         # page encoding: float32 models store float32; bf16 models store bf16-rounded values as float16 bits
         td = torch.float32 if desc["dtype"] == B.BS_F32 else torch.float16
         P = B.BS_PAGE_TOKENS
-        caps = [int(max_ctx)] * n_slots if slot_tokens is None else [int(t) for t in slot_tokens]
-        assert len(caps) == n_slots
-        pages_of = [(c + P - 1) // P for c in caps]
-        self.max_pages = max(pages_of)
+        self.block_table, self.n_pages = page_table(n_slots, max_ctx, slot_tokens, page_perm_seed, self.device)
+        self.max_pages = self.block_table.shape[1]
         self.n_slots = n_slots
-        self.n_pages = sum(pages_of)
         page_elems = desc["n_kv_heads"] * P * desc["head_dim"]
         # pages are zero-initialised: masked positions still enter the P*V product with weight 0
         self.k_pages = [torch.zeros(self.n_pages, page_elems, dtype=td, device=self.device)
                         for _ in range(desc["n_layers"])]
         self.v_pages = [torch.zeros(self.n_pages, page_elems, dtype=td, device=self.device)
                         for _ in range(desc["n_layers"])]
-        ids = torch.arange(self.n_pages, dtype=torch.int32)
-        if page_perm_seed is not None:      # scatter pages to exercise the block table
-            g = torch.Generator().manual_seed(page_perm_seed)
-            ids = ids[torch.randperm(self.n_pages, generator=g)]
-        table = torch.full((n_slots, self.max_pages), -1, dtype=torch.int32)
-        at = 0
-        for b, n in enumerate(pages_of):
-            table[b, :n] = ids[at:at + n]
-            at += n
-        self.block_table = table.contiguous().to(self.device)
         self.ctx_len = torch.zeros(n_slots, dtype=torch.int32, device=self.device)
         nbytes = B.bs_workspace_bytes(self.cdesc, B_max, k_max)
         if nbytes == 0:
@@ -164,3 +171,87 @@ class Engine:
 
     def poll_status(self):
         return B.bs_poll_status(self.ctx)
+
+
+class KvqCache:
+    """Owns a KV cache in 8 bits (pages, scales and block table of every layer, attention workspace) and forwards to bs_kvq_*.
+    Slots, capacities and page permutation as in Engine.  Rows are packed in batch order; n_max / q_max bound the rows of a
+    sequence, which are on the device.  `status` (one int32 on the device) collects BS_FAULT_* bits until poll_status."""
+
+    def __init__(self, n_layers, n_q_heads, n_kv_heads, head_dim, n_slots, max_ctx, q_max, device="cuda:0", page_perm_seed=None,
+                 slot_tokens=None):
+        self.device = torch.device(device)
+        self.n_q_heads, self.n_kv_heads, self.head_dim, self.n_slots, self.q_max = n_q_heads, n_kv_heads, head_dim, n_slots, q_max
+        self.block_table, self.n_pages = page_table(n_slots, max_ctx, slot_tokens, page_perm_seed, self.device)
+        page = n_kv_heads * B.BS_PAGE_TOKENS * head_dim
+        zeros = lambda *shape, dtype: [torch.zeros(*shape, dtype=dtype, device=self.device) for _ in range(n_layers)]
+        # zero-filled: masked positions still enter the P*V product with weight 0
+        self.k_pages, self.v_pages = zeros(self.n_pages, page, dtype=torch.uint8), zeros(self.n_pages, page, dtype=torch.uint8)
+        self.k_scale, self.v_scale = zeros(self.n_pages, n_kv_heads, dtype=torch.float32), zeros(self.n_pages, n_kv_heads, dtype=torch.float32)
+        self.desc = [B.make_kvq_desc(dict(n_pages=self.n_pages, n_slots=n_slots, max_pages_per_seq=self.block_table.shape[1], n_kv_heads=n_kv_heads,
+                                          head_dim=head_dim, k_pages=self.k_pages[l], v_pages=self.v_pages[l], k_scale=self.k_scale[l],
+                                          v_scale=self.v_scale[l], block_table=self.block_table)) for l in range(n_layers)]
+        nbytes = B.bs_kvq_workspace_bytes(n_q_heads, n_kv_heads, head_dim, q_max)
+        if nbytes == 0:
+            raise B.BsError(B.BS_ESHAPE, "bs_kvq_workspace_bytes rejected the shape")
+        self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+
+    def write(self, layer, seq_slot, pos0, n_rows, n_max, k_rows, v_rows):
+        """k_rows, v_rows: bf16 [rows, n_kv_heads, head_dim], to positions pos0[b] .. of slot seq_slot[b]."""
+        B.bs_kvq_write(self.desc[layer], seq_slot.numel(), seq_slot, pos0, n_rows, n_max, k_rows, v_rows, self.status)
+
+    def read(self, layer, seq_slot, pos0, n_rows, n_max, total):
+        """The values held of `total` rows in all, bf16 [total, n_kv_heads, head_dim]."""
+        k = torch.empty(total, self.n_kv_heads, self.head_dim, dtype=torch.bfloat16, device=self.device)
+        v = torch.empty_like(k)
+        B.bs_kvq_read(self.desc[layer], seq_slot.numel(), seq_slot, pos0, n_rows, n_max, k, v, self.status)
+        return k, v
+
+    def attention(self, layer, q, seq_slot, ctx_len, q_len, q_max, out=None):
+        """q: bf16 [rows, n_q_heads, head_dim]; row i of sequence b sees positions 0 .. ctx_len[b] + i."""
+        if q_max > self.q_max:
+            raise B.BsError(B.BS_ECAPACITY, "KvqCache.attention: q_max exceeds that of the workspace")
+        if out is None:
+            out = torch.empty(q.shape[0], self.n_q_heads, self.head_dim, dtype=torch.bfloat16, device=self.device)
+        B.bs_kvq_attention(self.desc[layer], seq_slot.numel(), seq_slot, ctx_len, q_len, q_max, self.n_q_heads, q, out, self.workspace, self.status)
+        return out
+
+    def poll_status(self):
+        fault = int(self.status.item())
+        self.status.zero_()
+        return fault
+
+
+class LogprobScorer:
+    """Owns the workspace of bs_token_logprobs for up to B_max sequences of k_max + 1 rows."""
+
+    def __init__(self, B_max, k_max, vocab, n_top, device="cuda:0"):
+        self.B_max, self.k_max, self.vocab, self.n_top = B_max, k_max, vocab, n_top
+        self.device = torch.device(device)
+        nbytes = B.bs_token_logprobs_workspace_bytes(B_max, k_max, vocab, n_top)
+        if nbytes == 0:
+            raise B.BsError(B.BS_ESHAPE, "bs_token_logprobs_workspace_bytes rejected the sizes")
+        self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+
+    def __call__(self, logits, tokens, n_tokens=None, draft_len=None, temperature=1.0):
+        """logits [rows, vocab] (float32 or bf16, packed); tokens [B, k_max + 1]; n_tokens, draft_len [B] or None (all rows).
+        Returns logprob, entropy [B, k_max + 1] and, with n_top, top_tokens, top_logprobs [B, k_max + 1, n_top]."""
+        n, width = tokens.shape
+        if n > self.B_max or width > self.k_max + 1 or logits.shape[1] != self.vocab:
+            raise B.BsError(B.BS_ESHAPE, "LogprobScorer: sizes exceed those of the workspace")
+        if draft_len is None and logits.shape[0] < n * width:
+            raise B.BsError(B.BS_ESHAPE, "LogprobScorer: fewer rows of logits than tokens")
+        new = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device=self.device)
+        out = {"logprob": new(n, width), "entropy": new(n, width)}
+        if self.n_top:
+            out["top_tokens"], out["top_logprobs"] = new(n, width, self.n_top, dtype=torch.int32), new(n, width, self.n_top)
+        B.bs_token_logprobs(n, self.vocab, logits, draft_len, width - 1, tokens, n_tokens, float(temperature), self.n_top, out["logprob"], out["entropy"],
+                            out.get("top_tokens"), out.get("top_logprobs"), self.workspace, self.status)
+        return out
+
+    def poll_status(self):
+        fault = int(self.status.item())
+        self.status.zero_()
+        return fault

@@ -1,0 +1,222 @@
+"""8-bit KV cache against its fp64 oracle: what is held after writes in every order is equal to the bit, attention is within the
+roundings of its operands and result."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kvq as O
+from paper_2605_08862_amd import binding as B
+from paper_2605_08862_amd.runtime import KvqCache
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _i32(v):
+    return torch.tensor(list(v), dtype=torch.int32, device=DEV)
+
+
+def _rows(rng, n, H, D, size=1.0):
+    x = rng.normal(0, size, (n, H, D))
+    if n:
+        x[:, :, 3] *= 7.0
+        x[rng.integers(n), :, :] *= 2.0 ** rng.integers(-12, 7)
+    return torch.from_numpy(x).to(torch.bfloat16)
+
+
+class Both:
+    """A cache and its oracle, written alike."""
+
+    def __init__(self, Hq, Hkv, D, caps, q_max, seed=0):
+        self.dims, self.caps = (Hq, Hkv, D), caps
+        self.cache = KvqCache(1, Hq, Hkv, D, len(caps), max(caps), q_max, device=DEV, page_perm_seed=seed, slot_tokens=caps)
+        self.k = [O.Slot(Hkv, D, c) for c in caps]
+        self.v = [O.Slot(Hkv, D, c) for c in caps]
+        self.len = [0] * len(caps)
+
+    def write(self, slots, pos, counts, k, v, n_max=None):
+        self.cache.write(0, _i32(slots), _i32(pos), _i32(counts), n_max or max(max(counts), 1), k.to(DEV), v.to(DEV))
+        at = 0
+        for s, p, n in zip(slots, pos, counts):
+            self.k[s].write(p, k[at:at + n].double().numpy())
+            self.v[s].write(p, v[at:at + n].double().numpy())
+            self.len[s] = p + n if n else self.len[s]
+            at += n
+
+    def check(self):
+        slots = list(range(len(self.caps)))
+        if sum(self.len) == 0:
+            return
+        k, v = self.cache.read(0, _i32(slots), _i32([0] * len(slots)), _i32(self.len), max(self.len), sum(self.len))
+        at = 0
+        for s, n in zip(slots, self.len):
+            for got, want in ((k, self.k[s]), (v, self.v[s])):
+                g = got[at:at + n].double().cpu().numpy()
+                assert np.array_equal(g, want.read(0, n)), (s, np.argwhere(g != want.read(0, n))[:4])
+            at += n
+        assert self.cache.poll_status() == 0
+
+
+@pytest.mark.parametrize("Hkv,D", [(1, 64), (2, 128), (4, 64), (3, 128)])
+def test_what_is_held_after_writes_in_every_order(Hkv, D):
+    rng = np.random.default_rng(Hkv * 100 + D)
+    caps = [70, 500, 64, 193, 300, 1]
+    x = Both(Hkv, Hkv, D, caps, 1, seed=3)
+
+    def step(slots, pos, counts, size=1.0):
+        n = sum(counts)
+        x.write(slots, pos, counts, _rows(rng, n, Hkv, D, size), _rows(rng, n, Hkv, D, size))
+        x.check()
+    step([1, 0, 4, 3], [0, 0, 0, 0], [300, 1, 64, 129])                     # prompts, whole and odd pages
+    step([0, 1, 2, 3, 4, 5], [1, 300, 0, 129, 64, 0], [17, 5, 63, 9, 0, 1])  # verify blocks, one sequence without rows
+    step([3, 0], [135, 18], [1, 1], size=40.0)                              # rejected rows are written over; scales grow
+    step([4, 1, 2], [64, 305, 63], [70, 20, 1], size=1e-3)                  # small rows behind large ones
+    step([1], [128], [200], size=0.1)                                       # a page begun anew takes a smaller scale again
+    step([0], [40], [30])                                                   # (rows 19 .. 39 were never written: what is there counts as 0)
+    for i in range(6):                                                      # row by row across a page's end
+        step([4, 3], [134 + i, 136 + i], [1, 1], size=2.0 ** i)
+
+
+def test_row_strides_and_unaligned_rows():
+    rng = np.random.default_rng(7)
+    H, D, n = 2, 128, 150
+    x = Both(H, H, D, [200], 1)
+    wide = torch.zeros(n, 3 * H * D + 5, dtype=torch.bfloat16)
+    k, v = _rows(rng, n, H, D), _rows(rng, n, H, D)
+    wide[:, 5:5 + H * D] = k.reshape(n, -1)
+    wide[:, 7 + H * D:7 + 2 * H * D] = v.reshape(n, -1)
+    dev = wide.to(DEV)
+    view = lambda a: dev[:, a:a + H * D].unflatten(1, (H, D))
+    B.bs_kvq_write(x.cache.desc[0], 1, _i32([0]), _i32([3]), _i32([n]), n, view(5), view(7 + H * D))
+    x.k[0].write(3, k.double().numpy())
+    x.v[0].write(3, v.double().numpy())
+    out = torch.full((n + 2, 2 * H * D + 2), 9.0, dtype=torch.bfloat16, device=DEV)
+    ko, vo = (out[:, a:a + H * D].unflatten(1, (H, D)) for a in (1, 1 + H * D))
+    B.bs_kvq_read(x.cache.desc[0], 1, _i32([0]), _i32([3]), _i32([n]), n, ko, vo)
+    assert np.array_equal(ko[:n].double().cpu().numpy(), x.k[0].read(3, n)) and np.array_equal(vo[:n].double().cpu().numpy(), x.v[0].read(3, n))
+    assert bool((out[n:] == 9.0).all()) and bool((out[:, 0] == 9.0).all()) and bool((out[:, -1] == 9.0).all())      # rows behind the last, left as they were
+
+
+def test_extremes():
+    H, D = 1, 64
+    for a in (0.0, 448.0, 450.0, 57344.0, 1e-30, 2.0 ** -24, 2.0 ** -20 * 1.0625, 1.75 * 2.0 ** -7, 1.7578125 * 2.0 ** -7):
+        x = Both(H, H, D, [64], 1)
+        rows = torch.full((3, H, D), a, dtype=torch.bfloat16)
+        rows[1] *= 0.37
+        x.write([0], [0], [3], rows, -rows)
+        x.check()
+    for a in (float("inf"), float("-inf"), float("nan"), 60000.0):
+        x = Both(H, H, D, [64], 1)
+        rows = torch.randn(5, H, D, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+        rows[2, 0, 7] = a
+        x.write([0], [0], [5], rows, rows.flip(0))
+        assert x.cache.poll_status() == B.BS_FAULT_RANGE
+        x.check()
+
+
+def test_faults_skip_the_sequence_and_nothing_else():
+    rng = np.random.default_rng(11)
+    H, D = 2, 64
+    x = Both(4, H, D, [130, 130, 130, 40], 4)
+    for s in range(3):
+        x.write([s], [0], [100], _rows(rng, 100, H, D), _rows(rng, 100, H, D))
+    x.check()
+    k, v = _rows(rng, 40, H, D), _rows(rng, 40, H, D)
+
+    def write(slots, pos, counts, n_max=30):
+        x.cache.write(0, _i32(slots), _i32(pos), _i32(counts), n_max, k.to(DEV), v.to(DEV))
+        return x.cache.poll_status()
+    assert write([0, 7], [100, 0], [0, 3]) == B.BS_FAULT_SLOT
+    assert write([-1], [0], [3]) == B.BS_FAULT_SLOT
+    assert write([-1], [0], [0]) == 0                                       # a padded entry
+    assert write([0], [-1], [3]) == B.BS_FAULT_KV_PAGES
+    assert write([0], [180], [30]) == B.BS_FAULT_KV_PAGES                   # 192 tokens in the table's width
+    assert write([3], [60], [5]) == B.BS_FAULT_KV_PAGES                     # second page is -1
+    assert write([0], [2 ** 31 - 2], [3]) == B.BS_FAULT_KV_PAGES
+    assert write([0, 1], [100, 100], [31, -1]) == B.BS_FAULT_DRAFT_LEN
+    x.check()
+    # of a slot used twice the first is written; rows of the skipped ones count in the packing, those of a bad count do not
+    got = write([0, 0, 9, 1, 2], [100, 50, 0, 100, 100], [3, 4, 2, 99, 5])
+    assert got == B.BS_FAULT_SLOT | B.BS_FAULT_DRAFT_LEN
+    for s, at, n in ((0, 0, 3), (2, 9, 5)):
+        x.k[s].write(100, k[at:at + n].double().numpy())
+        x.v[s].write(100, v[at:at + n].double().numpy())
+        x.len[s] = 100 + n
+    x.check()
+    # the same conditions in attention: rows of skipped sequences stay as they were
+    q = torch.randn(13, 4, D, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16)
+    out = torch.full((13, 4, D), 5.0, dtype=torch.bfloat16, device=DEV)
+    x.cache.attention(0, q.to(DEV), _i32([0, 9, 3, 2, 1, -1]), _i32([101, 0, 61, 103, 100, 0]), _i32([2, 4, 4, 2, 7, 0]), 4, out=out)
+    assert x.cache.poll_status() == B.BS_FAULT_SLOT | B.BS_FAULT_KV_PAGES | B.BS_FAULT_DRAFT_LEN
+    assert bool((out[2:10] == 5.0).all()) and bool((out[12:] == 5.0).all()) and not bool((out[:2] == 5.0).any()) and not bool((out[10:12] == 5.0).any())
+    for s, c, at in ((0, 101, 0), (2, 103, 10)):
+        _close(out[at:at + 2], q[at:at + 2], x.k[s].read(0, c + 2), x.v[s].read(0, c + 2), c)
+
+
+def _close(got, q, k, v, ctx):
+    """Half a step of bf16 for the result; per probability half a step of float16 (2^-11; below 2^-14, 2^-25) and what float32 leaves in its
+    score: D products and the scale, each 2^-24 of sum |q k| / sqrt(D), the subtracted maximum and the exponential 2^-20 of a score of less than 2^5
+    units; sums over t tokens in float32: t / 4 additions in each of at least four partial sums, and their merges."""
+    want, mag, most = O.attention(q.double().numpy(), k, v, ctx)
+    t = k.shape[0]
+    D = q.shape[2]
+    score = (D + 8) * 2.0 ** -24 * most + 2.0 ** -18
+    rel = 2.0 ** -11 + 2 * score + (t / 4 + 64) * 2.0 ** -24
+    tol = np.abs(want) * 2.0 ** -8 + 1.01 * rel * mag + 2.0 ** -25 * np.abs(v).max() * t * 0 + 2.0 ** -25 * np.abs(v).sum(0).max()
+    err = np.abs(got.double().cpu().numpy() - want)
+    assert np.all(err <= tol), (float((err / tol).max()), np.unravel_index((err / tol).argmax(), err.shape))
+
+
+CASES = [  # Hq, Hkv, D, contexts, rows
+    (1, 1, 64, [0], [1]),
+    (4, 4, 64, [128, 0, 63, 64], [5, 1, 1, 2]),
+    (6, 2, 128, [200, 31, 0, 500], [9, 0, 17, 3]),
+    (12, 2, 128, [1000], [1]),
+    (7, 1, 128, [95, 700, 1], [17, 1, 8]),
+    (28, 4, 128, [129, 640, 77], [1, 1, 1]),
+    (16, 2, 64, [300, 5], [16, 12]),
+    (128, 1, 64, [70, 0], [1, 3]),
+    (8, 8, 128, [1500, 33], [4, 31]),
+    (12, 2, 128, [0, 150], [130, 77]),
+    (4, 1, 64, [100, 0, 20], [200, 65, 1]),
+    (2, 2, 128, [3000, 10, 2900, 1, 64], [2, 2, 2, 2, 2]),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "q%d_kv%d_d%d_b%d_t%d_n%d" % (c[0], c[1], c[2], len(c[3]), max(c[3]), max(c[4])))
+def test_attention_matches_the_oracle(case):
+    Hq, Hkv, D, ctx, counts = case
+    rng = np.random.default_rng(Hq * 1000 + D + sum(ctx))
+    n = len(ctx)
+    slots = [int(s) for s in rng.permutation(n)]
+    caps = [0] * n
+    for b in range(n):
+        caps[slots[b]] = ctx[b] + counts[b] + 1
+    x = Both(Hq, Hkv, D, caps, max(counts), seed=5)
+    held = [c + r for c, r in zip(ctx, counts)]
+    x.write(slots, [0] * n, held, _rows(rng, sum(held), Hkv, D), _rows(rng, sum(held), Hkv, D, 0.5))
+    M = sum(counts)
+    q = torch.from_numpy(rng.normal(0, 1.0, (M, Hq, D))).to(torch.bfloat16)
+    out = torch.full((M + 3, Hq, D), 7.0, dtype=torch.bfloat16, device=DEV)
+    for _ in range(2):                                                      # twice on the same workspace
+        x.cache.attention(0, q.to(DEV), _i32(slots), _i32(ctx), _i32(counts), max(counts), out=out)
+        at = 0
+        for b in range(n):
+            s, r = slots[b], counts[b]
+            if r:
+                _close(out[at:at + r], q[at:at + r], x.k[s].read(0, held[b]), x.v[s].read(0, held[b]), ctx[b])
+            at += r
+        assert bool((out[M:] == 7.0).all()) and x.cache.poll_status() == 0
+    # strided queries, a larger q_max than needed, the same result
+    wide = torch.zeros(M, 2, Hq, D, dtype=torch.bfloat16, device=DEV)
+    wide[:, 1] = q.to(DEV)
+    again = torch.empty_like(out[:M])
+    big = KvqCache(1, Hq, Hkv, D, 1, 64, max(counts) + 40, device=DEV)
+    if max(counts) + 40 <= 64 * x.cache.block_table.shape[1]:
+        B.bs_kvq_attention(x.cache.desc[0], n, _i32(slots), _i32(ctx), _i32(counts), max(counts) + 40, Hq, wide[:, 1], again, big.workspace)
+        at = 0
+        for b in range(n):
+            s, r = slots[b], counts[b]
+            if r:
+                _close(again[at:at + r], q[at:at + r], x.k[s].read(0, held[b]), x.v[s].read(0, held[b]), ctx[b])
+            at += r

@@ -1,0 +1,135 @@
+"""bs_token_logprobs against its fp64 oracle."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import logprobs as O
+from paper_2605_08862_amd import binding as B
+from paper_2605_08862_amd.runtime import LogprobScorer
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+INF = float("inf")
+
+
+def _i32(v):
+    return torch.as_tensor(np.asarray(v), dtype=torch.int32, device=DEV)
+
+
+def _check(out, z, tokens, n_tokens, draft_len, temperature, n_top):
+    """y = (z - m) / T is off by 2^-23 of itself (a difference, a product with a rounded 1/T: 1.5 steps of 2^-24 each), the logarithm of the sum by
+    2^-23 of itself and by the sum's relative error: 3 * 2^-24 per exponential, its argument's, and additions of at most V / 256 terms in a row and a tree."""
+    z = z.double().cpu().numpy()
+    V, at = z.shape[1], 0
+    got = {k: v.double().cpu().numpy() if v.is_floating_point() else v.cpu().numpy() for k, v in out.items()}
+    for b in range(tokens.shape[0]):
+        for i in range(tokens.shape[1]):
+            if i >= n_tokens[b]:
+                assert got["logprob"][b, i] == 0 and got["entropy"][b, i] == 0
+                if n_top:
+                    assert (got["top_tokens"][b, i] == -1).all() and (got["top_logprobs"][b, i] == 0).all()
+                continue
+            row = z[at + i]
+            lp, h, top, ltop = O.row(row, tokens[b, i], temperature, n_top)
+            y = np.abs((row - row.max()) / temperature)[np.isfinite(row)] if np.isfinite(row).any() else np.zeros(1)
+            near = y[y < 100.0]
+            spread = near.max() if near.size else 0.0                     # terms further down are below 2^-144 of the sum
+            rel = 2.0 ** -24 * (4 + V / 256 + 16)
+            base = rel + 2.0 ** -22 * (1 + np.log(V))
+
+            def close(a, w, scale=1.0):
+                if np.isnan(w) or np.isinf(w):
+                    return (np.isnan(a) and np.isnan(w)) or a == w
+                if abs(w) > 3.4028235677973366e38:                        # beyond the largest float32 by half a step: infinite there
+                    return a == np.sign(w) * INF
+                return abs(a - w) <= scale * base + 2.0 ** -22 * abs(w) + 2.0 ** -22 * np.log(V)
+            assert close(got["logprob"][b, i], lp), (b, i, got["logprob"][b, i], lp)
+            # the weighted mean of y: an exponential's relative error times |y|, summed with weights p: at most (spread + 1) times the above
+            assert close(got["entropy"][b, i], h, 2.0 * (1.0 + min(spread, 2 * np.log(V) + 4))), (b, i, got["entropy"][b, i], h)
+            if n_top:
+                assert np.array_equal(got["top_tokens"][b, i], top), (b, i, got["top_tokens"][b, i], top)
+                assert all(close(a, w) for a, w in zip(got["top_logprobs"][b, i], ltop)), (got["top_logprobs"][b, i], ltop)
+        at += draft_len[b] + 1
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,n_top,temperature", [(2, 2, 1.0), (3, 0, 1.0), (33, 32, 0.7), (1000, 5, 1.3), (4096, 20, 1.0), (4999, 1, 0.5), (40001, 20, 0.8), (151936, 20, 1.0)])
+def test_ragged_rows(dtype, V, n_top, temperature):
+    rng = np.random.default_rng(V + n_top)
+    k_max, draft_len = 3, [3, 0, 2, 1, 3]
+    n_tokens = [4, 1, 2, 0, 3]
+    M = sum(k + 1 for k in draft_len)
+    z = torch.from_numpy(rng.normal(0, 2.5, (M, V)).astype(np.float32)).to(dtype)
+    if V >= 1000:
+        z[1, rng.random(V) < 0.5] = -INF                                  # a grammar's mask
+        z[2, rng.random(V) < 0.9] = torch.finfo(dtype).min
+        z[5, 5] += 60.0                                                   # a law that is nearly one token
+    z = z.to(DEV)
+    tokens = rng.integers(0, V, (5, k_max + 1))
+    s = LogprobScorer(5, k_max, V, n_top, device=DEV)
+    for _ in range(2):
+        out = s(z, _i32(tokens), _i32(n_tokens), _i32(draft_len), temperature)
+        _check(out, z, tokens, n_tokens, draft_len, temperature, n_top)
+    assert s.poll_status() == 0
+
+
+def test_ties_masks_and_rows_without_a_law():
+    V, n_top = 1000, 8
+    z = torch.zeros(9, V)
+    z[1] = -INF
+    z[2] = -INF
+    z[2, [7, 999]] = 3.0                                                  # two tokens left
+    z[3] = torch.finfo(torch.float32).min                                 # everything at the lowest value: a uniform law
+    z[4, ::3] = 1.0                                                       # more ties than alternatives
+    z[5, 13] = float("nan")
+    z[6, 500] = INF
+    z[7] = -0.0
+    z[7, 600:] = 0.0                                                      # -0 and 0 are equal
+    z[8] = -INF
+    z[8, 77] = -1e30                                                      # one token left, far down
+    tokens = np.array([[5], [5], [7], [0], [3], [2], [500], [1], [77]])
+    s = LogprobScorer(9, 0, V, n_top, device=DEV)
+    for dtype in (torch.float32, torch.bfloat16):
+        zd = z.to(dtype)
+        if dtype == torch.bfloat16:
+            zd[3] = torch.finfo(dtype).min
+        _check(s(zd.to(DEV), _i32(tokens)), zd, tokens, [1] * 9, [0] * 9, 1.0, n_top)
+    assert s.poll_status() == 0
+
+
+@pytest.mark.parametrize("V", [1001, 5003])
+def test_rows_that_start_anywhere(V):
+    """Odd vocabularies, and logits that start between sixteen-byte lines."""
+    rng = np.random.default_rng(V)
+    for dtype in (torch.float32, torch.bfloat16):
+        for skip in (0, 1, 3):
+            buf = torch.from_numpy(rng.normal(0, 2, 7 * V + skip).astype(np.float32)).to(dtype).to(DEV)
+            z = buf[skip:].view(7, V)
+            tokens = rng.integers(0, V, (7, 1))
+            tokens[0], tokens[1] = 0, V - 1
+            _check(LogprobScorer(7, 0, V, 6, device=DEV)(z, _i32(tokens)), z, tokens, [1] * 7, [0] * 7, 1.0, 6)
+
+
+def test_faults_and_optional_outputs():
+    V, k_max = 500, 2
+    rng = np.random.default_rng(5)
+    z = torch.from_numpy(rng.normal(0, 2, (9, V)).astype(np.float32)).to(DEV)
+    tokens = rng.integers(0, V, (5, 3))
+    s = LogprobScorer(5, k_max, V, 4, device=DEV)
+    bad = tokens.copy()
+    bad[0, 1], bad[2, 0] = V, -1
+    out = s(z, _i32(bad), _i32([3, 1, 3, 0, 0]), _i32([2, 0, 2, 0, 0]))
+    assert s.poll_status() == B.BS_FAULT_TOKEN_ID
+    assert out["logprob"][0, 1] == 0 and out["logprob"][2, 0] == 0 and (out["top_tokens"][0, 1] == -1).all() and out["logprob"][2, 1] != 0
+    # a bad draft_len counts no rows, a bad n_tokens skips its sequence only
+    dl, nt = [2, 7, 1, -1, 2], [3, 1, 3, 0, 3]
+    out = s(z, _i32(tokens), _i32(nt), _i32(dl))
+    assert s.poll_status() == B.BS_FAULT_DRAFT_LEN
+    keep = [0, 2, 4]
+    part = {k: v[keep] for k, v in out.items()}
+    _check(part, z, tokens[keep], [3, 0, 3], [2, 1, 2], 1.0, 4)
+    assert (out["logprob"][[1, 3]] == 0).all() and (out["top_tokens"][[1, 3]] == -1).all()
+    lp = torch.empty(3, 3, device=DEV)
+    B.bs_token_logprobs(3, V, z, None, 2, _i32(tokens[:3]), None, 1.0, 0, lp, None, None, None, s.workspace)   # no status, no entropy, no alternatives
+    want = torch.log_softmax(z.double(), -1).view(3, 3, V).gather(2, torch.as_tensor(tokens[:3], device=DEV)[..., None])[..., 0]
+    assert torch.allclose(lp.double(), want, atol=1e-5)
