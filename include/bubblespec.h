@@ -278,7 +278,7 @@ bs_status bs_kv_read(bs_ctx* ctx, int layer, int slot, int pos0, int n, void* k_
  * clears; BS_FAULT_* bits are or-ed into it; may be NULL).  Rows are packed in batch order: sequence b has n[b] rows, which start
  * at sum_{b'<b} n[b'] (a count outside [0, n_max] sets BS_FAULT_DRAFT_LEN and counts as 0).  A sequence with a bad slot
  * (BS_FAULT_SLOT), or with positions or page ids outside the cache (BS_FAULT_KV_PAGES), is skipped: its rows of the outputs and
- * its pages stay as they are.  A sequence without rows is skipped whatever its slot is (padded batches). */
+ * its pages stay as they are (attention: rows that see a bad page id).  A sequence without rows is skipped whatever its slot is (padded batches). */
 typedef struct {
   int32_t n_pages, n_slots, max_pages_per_seq, n_kv_heads, head_dim;
   void* k_pages;              /* dev [n_pages] pages of n_kv_heads * BS_PAGE_TOKENS * head_dim bytes, 16-byte aligned; element  */
@@ -309,8 +309,8 @@ bs_status bs_kvq_read(const bs_kvq_desc* kv, int B, const int32_t* seq_slot, con
  * workspace (dev, 256-byte aligned, at least bs_kvq_workspace_bytes of the same n_q_heads, n_kv_heads, head_dim and of a q_max no
  * smaller) is zero-filled once before its first use; calls that share one must not overlap in time.
  * Errors: BS_EINVAL (null, q or out not on 16 bytes, q_stride not a multiple of 8, misaligned workspace), BS_ESHAPE (as above;
- * n_q_heads not a multiple of n_kv_heads or more than 128 to one, q_max outside [1, max_pages_per_seq * BS_PAGE_TOKENS]),
- * BS_ECAPACITY (workspace too small), BS_EHIP. */
+ * n_q_heads not a multiple of n_kv_heads or more than 128 to one, q_max outside [1, max_pages_per_seq * BS_PAGE_TOKENS],
+ * B * n_kv_heads * (max_pages_per_seq / 2 + 1) * (q_max * n_q_heads / n_kv_heads / 128 + 1) above 2^30), BS_ECAPACITY (workspace too small), BS_EHIP. */
 size_t bs_kvq_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim, int q_max);   /* 0 on invalid arguments */
 bs_status bs_kvq_attention(const bs_kvq_desc* kv, int B, const int32_t* seq_slot /*[B]*/, const int32_t* ctx_len /*[B]*/,
                            const int32_t* q_len /*[B]*/, int q_max, int n_q_heads, const void* q, int64_t q_stride, void* out,
