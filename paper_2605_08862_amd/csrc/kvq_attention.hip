@@ -37,14 +37,213 @@ __device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
 #endif
 }
 
-// STEP: inside bs_verify_step (float16 queries, output in chunk order).
+// ---- the shares ------------------------------------------------------------------------------------------------------------------
+// Steps of the block of RP rows at qb of a sequence of n rows behind c tokens: of the tokens that its last row sees.
+template <int RP> __device__ __forceinline__ int block_steps(int c, int n, int G, int qb) { return (c + min(n - 1, ((qb + 1) * RP - 1) / G) + kStep) / kStep; }
+
+struct Share { int x, x_end, size, b; };               // steps [x, x_end) of all, the length of a share, the sequence of step x
+
+// Called by all threads.  s_start, s_row [B + 1]: first step and first packed row of every sequence; s_scan: 3 words for each wave.
+// A share is no shorter than sqrt(steps of the longest unit * merge_cost / 16), since its partials have to be merged by one workgroup.
+template <int THREADS, int RP>
+__device__ __forceinline__ Share find_share(const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
+                                            int n_max, int B, int n_slots, int max_pages, int G, int Hkv, int merge_cost, int* s_start, int* s_row, int* s_scan,
+                                            int32_t* __restrict__ status) {
+  constexpr int W = THREADS / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (B + THREADS - 1) / THREADS, lo = min(tid * per, B), hi = min(lo + per, B);
+  int steps = 0, rows = 0, fault = 0, most = 0;
+  for (int b = lo; b < hi; ++b) {
+    s_start[b] = steps;
+    s_row[b] = rows;
+    const int n = seq_n[b] + n_add, slot = seq_slot[b], c = seq_pos[b];
+    if (n < 0 || n > n_max) { fault |= BS_FAULT_DRAFT_LEN; continue; }
+    if (n == 0) continue;
+    rows += n;
+    if (slot < 0 || slot >= n_slots) { fault |= BS_FAULT_SLOT; continue; }
+    if (c < 0 || (long long)c + n > (long long)max_pages * kPage) { fault |= BS_FAULT_KV_PAGES; continue; }
+    const int blocks = (n * G + RP - 1) / RP;
+    int s = 0;
+    for (int qb = 0; qb < blocks; ++qb) s += block_steps<RP>(c, n, G, qb);
+    most = max(most, block_steps<RP>(c, n, G, blocks - 1));
+    steps += s * Hkv;
+  }
+  if (fault && blockIdx.x == 0 && status) atomicOr(status, fault);
+  int is = steps, ir = rows;                            // exclusive prefix over the threads
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int a = __shfl_up(is, o), r = __shfl_up(ir, o);
+    if (lane >= o) { is += a; ir += r; }
+    most = max(most, __shfl_xor(most, o));
+  }
+  if (lane == 63) { s_scan[wave] = is; s_scan[W + wave] = ir; s_scan[2 * W + wave] = most; }
+  __syncthreads();
+  int bs = is - steps, br = ir - rows, total = 0;
+  most = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    if (w < wave) { bs += s_scan[w]; br += s_scan[W + w]; }
+    total += s_scan[w];
+    most = max(most, s_scan[2 * W + w]);
+  }
+  for (int b = lo; b < hi; ++b) { s_start[b] += bs; s_row[b] += br; }
+  if (tid == 0) s_start[B] = total;
+  __syncthreads();
+  total = __builtin_amdgcn_readfirstlane(total);
+  int size = max((total + (int)gridDim.x - 1) / (int)gridDim.x, (int)sqrtf((float)most * (float)merge_cost * 0.0625f));
+  size = __builtin_amdgcn_readfirstlane(max(size, 1));
+  Share sh{(int)blockIdx.x * size, 0, size, 0};
+  sh.x_end = min(sh.x + size, total);
+  int top = B;                                          // largest b with s_start[b] <= x (sequences without steps are passed over)
+  while (top - sh.b > 1) { const int mid = (sh.b + top) >> 1; if (s_start[mid] <= sh.x) sh.b = mid; else top = mid; }
+  return sh;
+}
+
+// The unit that step x of a share lies in, and the part [s_lo, s_hi) of its steps that the share has.
+struct Unit {
+  int b, h, n, c, row0;                                 // sequence, KV head, its rows, the tokens before them, first packed row
+  int first, steps, s_lo, s_hi;                         // first step of the unit among all
+  int qr0, R, n_tiles, c_all;                           // first row (query row x head) of the block in the sequence, rows, tiles, last position that every row sees
+  bool whole;
+  int w_first, w_last;                                  // workgroups that have a part
+};
+template <int RP>
+__device__ __forceinline__ Unit find_unit(Share& sh, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
+                                          int G, int Hkv) {
+  while (s_start[sh.b + 1] <= sh.x) ++sh.b;
+  Unit u;
+  u.b = sh.b = __builtin_amdgcn_readfirstlane(sh.b);
+  u.n = seq_n[u.b] + n_add;
+  u.c = seq_pos[u.b];
+  u.row0 = __builtin_amdgcn_readfirstlane(s_row[u.b]);
+  const int first = __builtin_amdgcn_readfirstlane(s_start[u.b]);
+  const int per_head = __builtin_amdgcn_readfirstlane((s_start[u.b + 1] - first) / Hkv);
+  u.h = (sh.x - first) / per_head;
+  u.first = first + u.h * per_head;
+  int qb = 0;
+  for (int s; u.first + (s = block_steps<RP>(u.c, u.n, G, qb)) <= sh.x; ++qb) u.first += s;
+  u.steps = block_steps<RP>(u.c, u.n, G, qb);
+  u.s_lo = sh.x - u.first;
+  u.s_hi = min(u.steps, sh.x_end - u.first);
+  u.qr0 = qb * RP;
+  u.R = min(u.n * G - u.qr0, RP);
+  u.n_tiles = (u.c + min(u.n - 1, (u.qr0 + RP - 1) / G)) / kTile + 1;
+  u.c_all = u.c + u.qr0 / G;
+  u.whole = u.s_lo == 0 && u.s_hi == u.steps;
+  u.w_first = u.first / sh.size;
+  u.w_last = (u.first + u.steps - 1) / sh.size;
+  return u;
+}
+// Partial rows: two places for each workgroup, for a unit that began before its share and for one that goes on behind it.
+template <int RP> __device__ __forceinline__ uint32_t partial_row(int w, bool began_here) { return (uint32_t)(2 * w + (began_here ? 1 : 0)) * RP; }
+
+template <int D, bool STEP>
+__device__ __forceinline__ void store4(const KvqOut& out, int Hq, int row, int col, f32x4 v, float inv, int32_t* status) {
+  if constexpr (STEP) {
+    *(f16x4*)((f16*)out.p + act_index(row, col, out.ld)) = to_f16x4_guarded(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, status);
+  } else {
+    typedef bf16 b4 __attribute__((ext_vector_type(4)));
+    *(b4*)((bf16*)out.p + (size_t)row * Hq * D + col) = b4{(bf16)(v[0] * inv), (bf16)(v[1] * inv), (bf16)(v[2] * inv), (bf16)(v[3] * inv)};
+  }
+}
+
+// Merges the partials of a unit; called by the last of its workgroups to arrive.  An item is four columns of a row, eight partials in flight.
+template <int THREADS, int RP, int D, bool STEP>
+__device__ __forceinline__ void merge_unit(const Unit& un, const float* part_o, const float* part_ml, const KvqOut& out, int Hq, int G, int32_t* status) {
+  constexpr int CH = D / 4, GC = 8;
+  const wt_buf bo = wt_buffer(part_o), bm = wt_buffer(part_ml);
+  for (int it = threadIdx.x; it < un.R * CH; it += THREADS) {
+    const int r = it / CH, ch = it % CH;
+    float m = -INFINITY, l = 0.f;
+    f32x4 acc{0.f, 0.f, 0.f, 0.f};
+    for (int c0 = un.w_first; c0 <= un.w_last; c0 += GC) {
+      wt_f32x2 ml[GC];
+      f32x4 v[GC];
+#pragma unroll
+      for (int u = 0; u < GC; ++u) {
+        const int c = min(c0 + u, un.w_last);
+        const uint32_t pr = partial_row<RP>(c, c == un.w_first) + r;
+        ml[u] = wt_load2(bm, pr * 8);
+        v[u] = wt_load4(bo, (pr * D + ch * 4) * 4);
+      }
+      float mg = m;
+#pragma unroll
+      for (int u = 0; u < GC; ++u) mg = fmaxf(mg, ml[u][0]);
+      if (mg == -INFINITY) continue;
+      const float f0 = __builtin_amdgcn_exp2f(m - mg);
+      l *= f0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] *= f0;
+#pragma unroll
+      for (int u = 0; u < GC; ++u) {
+        const float f = c0 + u <= un.w_last ? __builtin_amdgcn_exp2f(ml[u][0] - mg) : 0.f;
+        l += ml[u][1] * f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += v[u][e] * f;
+      }
+      m = mg;
+    }
+    if (m == INFINITY) continue;                        // a bad page: the row stays as it is
+    const int qr = un.qr0 + r;
+    store4<D, STEP>(out, Hq, un.row0 + qr / G, (un.h * G + qr % G) * D + ch * 4, acc, 1.0f / l, status);
+  }
+}
+
+// Online softmax of one tile of scores (attn_softmax.h): the scores become probabilities in float16, the running maximum, sum and accumulators follow.
+template <int DT>
+__device__ __forceinline__ void softmax_tile(const f32x16& st, bool full, int tok0, int lim, float scale_log2e, float& m_run, float& l_run, f32x16 (&o)[DT], f16x8 (&pf)[2]) {
+  float y[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) y[i] = full || tok0 + i <= lim ? st[i] : -INFINITY;
+  float mloc = y[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) mloc = fmaxf(mloc, y[i]);
+  mloc = max_halves(mloc) * scale_log2e;                // scale > 0 commutes with max
+  if (__any(mloc > m_run + kLateRescale)) {
+    const float m_new = fmaxf(m_run, mloc);
+    const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+    l_run *= alpha;
+    m_run = m_new;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
+  }
+  const float m_safe = m_run == -INFINITY ? 0.f : m_run;
+  float psum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    y[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[i], scale_log2e, -m_safe));
+    psum += y[i];
+  }
+  l_run += psum;                                        // per half of the wave; the halves are added at the end
+#pragma unroll
+  for (int i = 0; i < 16; ++i) pf[i / 8][i % 8] = (f16)y[i];
+}
+
+// Sixteen bytes of a query row as float16.
+template <bool STEP> __device__ __forceinline__ u32x4 query8(u32x4 v, bool& range) {
+  if constexpr (STEP) return v;
+  const bf16x8 y = __builtin_bit_cast(bf16x8, v);
+  f16x8 z;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float f = (float)y[e];
+    if (!(fabsf(f) <= 65504.f)) { f = f16_saturate(f); range = true; }
+    z[e] = (f16)f;
+  }
+  return __builtin_bit_cast(u32x4, z);
+}
+
+#define BS_KVQ_PARAMS                                                                                                                                     \
+  const int32_t *__restrict__ seq_slot, const int32_t *__restrict__ seq_pos, const int32_t *__restrict__ seq_n, int n_add, int n_max, int B,                \
+      const int32_t *__restrict__ block_table, int n_slots, int max_pages, int n_pages, const uint8_t *__restrict__ k_pages, const uint8_t *__restrict__ v_pages, \
+      const float *__restrict__ k_scale, const float *__restrict__ v_scale, int Hq, int Hkv, float scale_log2e, const uint16_t *__restrict__ q, size_t q_stride, \
+      KvqOut out, int merge_cost, float *__restrict__ part_o, float *__restrict__ part_ml, int32_t *__restrict__ counters, int32_t *__restrict__ status
+
+// Blocks of up to 32 NQ rows, four waves.  STEP: inside bs_verify_step (float16 queries, output in chunk order).
 template <int NQ, int D, bool STEP>
-__global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1)
-kvq_attention_kernel(const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add, int n_max, int B,
-                     const int32_t* __restrict__ block_table, int n_slots, int max_pages, int n_pages, const uint8_t* __restrict__ k_pages,
-                     const uint8_t* __restrict__ v_pages, const float* __restrict__ k_scale, const float* __restrict__ v_scale, int Hq, int Hkv,
-                     float scale_log2e, const uint16_t* __restrict__ q, size_t q_stride, KvqOut out, int share_min_num, float* __restrict__ part_o,
-                     float* __restrict__ part_ml, int32_t* __restrict__ counters, int32_t* __restrict__ status) {
+__global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) kvq_attention_kernel(BS_KVQ_PARAMS) {
   constexpr int KS = D / 16, DT = D / 32, RP = 32 * NQ, CH = D / 4;
   constexpr int LDO = D + 4;                            // row stride (floats) of an accumulator in LDS
   extern __shared__ __align__(16) char lds_raw[];
@@ -54,145 +253,24 @@ kvq_attention_kernel(const int32_t* __restrict__ seq_slot, const int32_t* __rest
   constexpr size_t kOBytes = (size_t)4 * 32 * LDO * 4, kQBytes = (size_t)NQ * KS * 1024;
   float* const s_m = (float*)(lds_raw + (kOBytes > kQBytes ? kOBytes : kQBytes));   // [4][NQ * 32]
   float* const s_l = s_m + 4 * RP;
-  int* const s_start = (int*)(s_l + 4 * RP);            // [B + 1] first step of every sequence
-  int* const s_row = s_start + B + 1;                   // [B + 1] first packed row
-  const int tid = threadIdx.x, G = Hq / Hkv;
+  int* const s_start = (int*)(s_l + 4 * RP);            // [B + 1]
+  int* const s_row = s_start + B + 1;                   // [B + 1]
+  const int tid = threadIdx.x, G = Hq / Hkv, w_id = blockIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, ln = lane & 31, lg = lane >> 5;
-
-  // ---- the shares --------------------------------------------------------------------------------------------------------------
-  auto block_steps = [&](int c, int n, int qb) { return (c + min(n - 1, ((qb + 1) * RP - 1) / G) + kStep) / kStep; };   // of the tokens that the block's last row sees
-  int most = 0;
-  {
-    const int per = (B + 255) / 256, lo = min(tid * per, B), hi = min(lo + per, B);
-    int steps = 0, rows = 0, fault = 0;
-    for (int b = lo; b < hi; ++b) {
-      s_start[b] = steps;
-      s_row[b] = rows;
-      const int n = seq_n[b] + n_add;
-      if (n < 0 || n > n_max) { fault |= BS_FAULT_DRAFT_LEN; continue; }
-      if (n == 0) continue;
-      rows += n;
-      const int slot = seq_slot[b], c = seq_pos[b];
-      if (slot < 0 || slot >= n_slots) { fault |= BS_FAULT_SLOT; continue; }
-      if (c < 0 || (long long)c + n > (long long)max_pages * kPage) { fault |= BS_FAULT_KV_PAGES; continue; }
-      const int blocks = (n * G + RP - 1) / RP;
-      int s = 0;
-      for (int qb = 0; qb < blocks; ++qb) s += block_steps(c, n, qb);
-      most = max(most, block_steps(c, n, blocks - 1));
-      steps += s * Hkv;
-    }
-    if (fault && blockIdx.x == 0 && status) atomicOr(status, fault);
-    // exclusive prefix over the threads
-    int is = steps, ir = rows;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int a = __shfl_up(is, o), r = __shfl_up(ir, o);
-      if (lane >= o) { is += a; ir += r; }
-      most = max(most, __shfl_xor(most, o));
-    }
-    if (lane == 63) { s_scan[wave] = is; s_scan[4 + wave] = ir; }
-    if (lane == 0) s_scan[8 + wave] = most;
-    __syncthreads();
-    int bs = is - steps, br = ir - rows;
-#pragma unroll
-    for (int w = 0; w < 3; ++w) if (w < wave) { bs += s_scan[w]; br += s_scan[4 + w]; }
-    for (int b = lo; b < hi; ++b) { s_start[b] += bs; s_row[b] += br; }
-    if (tid == 0) { s_start[B] = s_scan[0] + s_scan[1] + s_scan[2] + s_scan[3]; s_row[B] = 0; }
-    most = max(max(s_scan[8], s_scan[9]), max(s_scan[10], s_scan[11]));
-    __syncthreads();
-  }
-  const int total = __builtin_amdgcn_readfirstlane(s_start[B]);
-  // a share is no shorter than sqrt(steps of the longest unit * share_min_num / 16): its partials have to be merged by one workgroup
-  int share = (total + (int)gridDim.x - 1) / (int)gridDim.x;
-  share = max(share, (int)sqrtf((float)most * (float)share_min_num * 0.0625f));
-  share = __builtin_amdgcn_readfirstlane(max(share, 1));
-  const int w_id = blockIdx.x;
-  int x = w_id * share;
-  const int x_end = min(x + share, total);
-  if (x >= x_end) return;
-  int b = 0;
-  {
-    int hi = B;                                         // largest b with s_start[b] <= x (sequences without steps are passed over)
-    while (hi - b > 1) { const int mid = (b + hi) >> 1; if (s_start[mid] <= x) b = mid; else hi = mid; }
-    b = __builtin_amdgcn_readfirstlane(b);
-  }
-
-  auto store4 = [&](int row, int col, f32x4 v) {
-    if constexpr (STEP) {
-      *(f16x4*)((f16*)out.p + act_index(row, col, out.ld)) = to_f16x4_guarded(v[0], v[1], v[2], v[3], status);
-    } else {
-      typedef bf16 b4 __attribute__((ext_vector_type(4)));
-      *(b4*)((bf16*)out.p + (size_t)row * Hq * D + col) = b4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
-    }
-  };
-
-  // Merges the partials of a unit, workgroups w0 .. w1: an item is four columns of a row.
-  auto merge_unit = [&](int w0, int w1, int R, int row0, int qr0, int h) {
-    const wt_buf bo = wt_buffer(part_o), bm = wt_buffer(part_ml);
-    for (int it = tid; it < R * CH; it += 256) {
-      const int r = it / CH, ch = it % CH;
-      float m = -INFINITY, l = 0.f;
-      f32x4 acc{0.f, 0.f, 0.f, 0.f};
-      constexpr int GC = 8;
-      for (int c0 = w0; c0 <= w1; c0 += GC) {
-        wt_f32x2 ml[GC];
-        f32x4 v[GC];
-#pragma unroll
-        for (int u = 0; u < GC; ++u) {
-          const int c = min(c0 + u, w1);
-          const uint32_t pr = (uint32_t)(2 * c + (c == w0 ? 1 : 0)) * RP + r;
-          ml[u] = wt_load2(bm, pr * 8);
-          v[u] = wt_load4(bo, (pr * D + ch * 4) * 4);
-        }
-        float mg = m;
-#pragma unroll
-        for (int u = 0; u < GC; ++u) mg = fmaxf(mg, ml[u][0]);
-        if (mg == -INFINITY) continue;
-        const float f0 = __builtin_amdgcn_exp2f(m - mg);
-        l *= f0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] *= f0;
-#pragma unroll
-        for (int u = 0; u < GC; ++u) {
-          if (c0 + u > w1) break;
-          const float f = __builtin_amdgcn_exp2f(ml[u][0] - mg);
-          l += ml[u][1] * f;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[e] += v[u][e] * f;
-        }
-        m = mg;
-      }
-      if (m == INFINITY) continue;                      // a bad page: the row stays as it is
-      const float inv = 1.0f / l;
-      const int qr = qr0 + r;
-      store4(row0 + qr / G, (h * G + qr % G) * D + ch * 4, f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv});
-    }
-  };
-
-  // ---- the units of the share --------------------------------------------------------------------------------------------------
-  while (x < x_end) {
-    while (s_start[b + 1] <= x) ++b;
-    b = __builtin_amdgcn_readfirstlane(b);
-    const int n = seq_n[b] + n_add, c = seq_pos[b], row0 = __builtin_amdgcn_readfirstlane(s_row[b]);
-    const int first = __builtin_amdgcn_readfirstlane(s_start[b]);
-    const int per_head = __builtin_amdgcn_readfirstlane((s_start[b + 1] - first) / Hkv);
-    const int h = (x - first) / per_head;
-    int unit = first + h * per_head, qb = 0;            // first step of the unit
-    for (int s; unit + (s = block_steps(c, n, qb)) <= x; ++qb) unit += s;
-    const int steps = block_steps(c, n, qb), s_lo = x - unit, s_hi = min(steps, x_end - unit);
-    const int qr0 = qb * RP, R = min(n * G - qr0, RP);  // packed query rows of the block
-    const int32_t* __restrict__ bt = block_table + (size_t)seq_slot[b] * max_pages;
-    const int n_tok = c + min(n - 1, (qr0 + RP - 1) / G) + 1, n_tiles = (n_tok + kTile - 1) / kTile;
-    const int t0 = 4 * s_lo + wave, t_end = min(4 * s_hi, n_tiles);
+  Share sh = find_share<256, RP>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, merge_cost, s_start, s_row, s_scan, status);
+  while (sh.x < sh.x_end) {
+    const Unit un = find_unit<RP>(sh, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv);
+    const int32_t* __restrict__ bt = block_table + (size_t)seq_slot[un.b] * max_pages;
+    const int t0 = 4 * un.s_lo + wave, t_end = min(4 * un.s_hi, un.n_tiles);
     const int n_my = t0 < t_end ? (t_end - t0 + 3) / 4 : 0, t_last = t0 + (n_my - 1) * 4;
-    const int c_all = c + qr0 / G;                      // last position that every row sees
     bool bad = false;
 
     struct At { size_t off; float ks, vs; };
     auto place = [&](int t) -> At {
       int page = bt[t * kTile / kPage];
       if ((unsigned)page >= (unsigned)n_pages) { page = 0; bad = true; }
-      return At{(size_t)page * ((size_t)Hkv * kPage * D) + (size_t)(h * 2 + (t & 1)) * (kTile * D) + lane * 16, k_scale[(size_t)page * Hkv + h], v_scale[(size_t)page * Hkv + h]};
+      return At{(size_t)page * ((size_t)Hkv * kPage * D) + (size_t)(un.h * 2 + (t & 1)) * (kTile * D) + lane * 16, k_scale[(size_t)page * Hkv + un.h],
+                v_scale[(size_t)page * Hkv + un.h]};
     };
     auto load_tile = [&](const uint8_t* base, size_t off, u32x4 (&f)[DT]) {
 #pragma unroll
@@ -205,31 +283,18 @@ kvq_attention_kernel(const int32_t* __restrict__ seq_slot, const int32_t* __rest
 #pragma unroll
     for (int j = 0; j < QF; ++j) {
       const int f = wave + 4 * j, qt = f / KS, s = f % KS;
-      const int qr = qr0 + min(qt * 32 + ln, R - 1);    // rows behind the last one are masked
-      qv[j] = *(const u32x4*)(q + (size_t)(row0 + qr / G) * q_stride + (size_t)(h * G + qr % G) * D + lg * (D / 2) + s * 8);
+      const int qr = un.qr0 + min(qt * 32 + ln, un.R - 1);    // rows behind the last one are masked
+      qv[j] = *(const u32x4*)(q + (size_t)(un.row0 + qr / G) * q_stride + (size_t)(un.h * G + qr % G) * D + lg * (D / 2) + s * 8);
     }
     u32x4 k0[DT], v0[DT], k1[DT], v1[DT];
-    At a0 = place(n_my > 0 ? t0 : n_tiles - 1), a1 = place(n_my > 1 ? t0 + 4 : n_my > 0 ? t0 : n_tiles - 1);
+    At a0 = place(n_my > 0 ? t0 : un.n_tiles - 1), a1 = place(n_my > 1 ? t0 + 4 : n_my > 0 ? t0 : un.n_tiles - 1);
     load_tile(k_pages, a0.off, k0);
     load_tile(v_pages, a0.off, v0);
     load_tile(k_pages, a1.off, k1);
     load_tile(v_pages, a1.off, v1);
     bool range = false;
 #pragma unroll
-    for (int j = 0; j < QF; ++j) {
-      if constexpr (!STEP) {
-        const bf16x8 y = __builtin_bit_cast(bf16x8, qv[j]);
-        f16x8 z;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float f = (float)y[e];
-          if (!(fabsf(f) <= 65504.f)) { f = f16_saturate(f); range = true; }
-          z[e] = (f16)f;
-        }
-        qv[j] = __builtin_bit_cast(u32x4, z);
-      }
-      s_q[(wave + 4 * j) * 64 + lane] = qv[j];
-    }
+    for (int j = 0; j < QF; ++j) s_q[(wave + 4 * j) * 64 + lane] = query8<STEP>(qv[j], range);
     if (range && status) atomicOr(status, BS_FAULT_RANGE);
     __syncthreads();
     const u32x4* my_q = s_q + lane;
@@ -241,7 +306,7 @@ kvq_attention_kernel(const int32_t* __restrict__ seq_slot, const int32_t* __rest
     for (int qt = 0; qt < NQ; ++qt) {
       m_run[qt] = -INFINITY;
       l_run[qt] = 0.f;
-      lim[qt] = qt * 32 + ln < R ? c + (qr0 + qt * 32 + ln) / G : -1;
+      lim[qt] = qt * 32 + ln < un.R ? un.c + (un.qr0 + qt * 32 + ln) / G : -1;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -252,8 +317,6 @@ kvq_attention_kernel(const int32_t* __restrict__ seq_slot, const int32_t* __rest
       constexpr bool PREF = decltype(pref)::value;
       At next{0, 1.f, 1.f};
       if (PREF) next = place(t_pref);
-      const int tok0 = t * kTile + 16 * lg;             // accumulator register i <-> token tok0 + i
-      const bool full = (t + 1) * kTile - 1 <= c_all;
       f32x16 st[NQ];
 #pragma unroll
       for (int qt = 0; qt < NQ; ++qt)
@@ -270,34 +333,8 @@ kvq_attention_kernel(const int32_t* __restrict__ seq_slot, const int32_t* __rest
       __builtin_amdgcn_sched_barrier(0);
       f16x8 pf[NQ][2];
 #pragma unroll
-      for (int qt = 0; qt < NQ; ++qt) {
-        float y[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) y[i] = full || tok0 + i <= lim[qt] ? st[qt][i] : -INFINITY;
-        float mloc = y[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) mloc = fmaxf(mloc, y[i]);
-        mloc = max_halves(mloc) * scale_log2e;          // scale > 0 commutes with max
-        if (__any(mloc > m_run[qt] + kLateRescale)) {
-          const float m_new = fmaxf(m_run[qt], mloc);
-          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[qt] - m_new);
-          l_run[qt] *= alpha;
-          m_run[qt] = m_new;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[qt][dt][i] *= alpha;
-        }
-        const float m_safe = m_run[qt] == -INFINITY ? 0.f : m_run[qt];
-        float psum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          y[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[i], scale_log2e, -m_safe));
-          psum += y[i];
-        }
-        l_run[qt] += psum;                              // per half of the wave; the halves are added at the end
-#pragma unroll
-        for (int i = 0; i < 16; ++i) pf[qt][i / 8][i % 8] = (f16)y[i];
+      for (int qt = 0; qt < NQ; ++qt) {                  // accumulator register i <-> token t * kTile + 16 lg + i
+        softmax_tile<DT>(st[qt], (t + 1) * kTile - 1 <= un.c_all, t * kTile + 16 * lg, lim[qt], scale_log2e, m_run[qt], l_run[qt], o[qt], pf[qt]);
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
@@ -323,10 +360,8 @@ kvq_attention_kernel(const int32_t* __restrict__ seq_slot, const int32_t* __rest
       if (i < n_my) tile(std::false_type{}, t0 + i * 4, 0, k0, v0, a0);
     }
 
-    // ---- merge of the waves, one query tile at a time --------------------------------------------------------------------------
-    const bool whole = s_lo == 0 && s_hi == steps;
-    const int w_first = unit / share, w_last = (unit + steps - 1) / share;
-    const uint32_t part = (uint32_t)(2 * w_id + (s_lo == 0 ? 1 : 0)) * RP;
+    // ---- merge of the waves, one query tile at a time
+    const uint32_t part = partial_row<RP>(w_id, un.s_lo == 0);
     const wt_buf bo = wt_buffer(part_o), bm = wt_buffer(part_ml);
     if (bad && lane == 0 && status) atomicOr(status, BS_FAULT_KV_PAGES);
 #pragma unroll
@@ -336,7 +371,7 @@ kvq_attention_kernel(const int32_t* __restrict__ seq_slot, const int32_t* __rest
     }
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
-      if (qt * 32 >= R) break;
+      if (qt * 32 >= un.R) break;
       __syncthreads();                                  // the fragments, or the accumulators of the tile before, are no longer read
       float* mine = s_o + (size_t)wave * 32 * LDO;
 #pragma unroll
@@ -345,7 +380,7 @@ kvq_attention_kernel(const int32_t* __restrict__ seq_slot, const int32_t* __rest
         for (int i4 = 0; i4 < 4; ++i4)
           *(f32x4*)(mine + ln * LDO + dt * 32 + 8 * i4 + 4 * lg) = f32x4{o[qt][dt][4 * i4], o[qt][dt][4 * i4 + 1], o[qt][dt][4 * i4 + 2], o[qt][dt][4 * i4 + 3]};
       __syncthreads();
-      for (int it = tid; it < min(R - qt * 32, 32) * CH; it += 256) {
+      for (int it = tid; it < min(un.R - qt * 32, 32) * CH; it += 256) {
         const int r = it / CH, ch = it % CH, rr = qt * 32 + r;
         float mw[4], mt = -INFINITY, lt = 0.f;
 #pragma unroll
@@ -360,58 +395,236 @@ kvq_attention_kernel(const int32_t* __restrict__ seq_slot, const int32_t* __rest
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] += v[e] * f;
           }
-        if (!whole) {
+        if (!un.whole) {
           wt_store4(bo, ((part + rr) * D + ch * 4) * 4, acc);
           if (ch == 0) wt_store2(bm, (part + rr) * 8, mt, lt);
         } else if (mt != INFINITY) {
-          const float inv = 1.0f / lt;
-          const int qr = qr0 + rr;
-          store4(row0 + qr / G, (h * G + qr % G) * D + ch * 4, f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv});
+          const int qr = un.qr0 + rr;
+          store4<D, STEP>(out, Hq, un.row0 + qr / G, (un.h * G + qr % G) * D + ch * 4, acc, 1.0f / lt, status);
         }
       }
     }
-    if (!whole && publish_arrival(counters + w_first, w_last - w_first + 1, &s_flag)) merge_unit(w_first, w_last, R, row0, qr0, h);
-    x = unit + s_hi;
+    if (!un.whole && publish_arrival(counters + un.w_first, un.w_last - un.w_first + 1, &s_flag)) merge_unit<256, RP, D, STEP>(un, part_o, part_ml, out, Hq, G, status);
+    sh.x = un.first + un.s_hi;
     __syncthreads();                                    // LDS is the next unit's
   }
 }
 
-// Query tiles of a block: what the rows of a sequence need, at most four (accumulators of four tiles of 32 rows x 128 fill half of the registers).
-int query_tiles(int G, int q_max) {
-  const long long rows = (long long)q_max * G;
-  return rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+// Waits until at most N of this wave's requests are in flight (and for its LDS accesses), then for the other waves.
+template <int N> __device__ __forceinline__ void wait_requests() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+#endif
 }
-int workgroups(int NQ) { return (NQ == 1 ? 2 : 1) * kCUs; }
+// A wave's sixteen bytes per lane from memory to 1 KiB of LDS (dst: the same in all lanes).
+__device__ __forceinline__ void copy_to_lds(const uint8_t* src, char* dst) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+#endif
+}
 
-template <int NQ, int D, bool STEP>
+// Blocks of up to 128 rows, eight waves: wave w has query tile w % NQT and token phase w / NQT, NQT = 2 or 4 tiles by the rows of the unit; the 8 / NQT phases
+// work on different token tiles.  The waves of a phase share a tile of codes in LDS: the memory pipeline copies it there (global -> LDS loads, a share of the
+// 1 KiB pieces by each wave), NB buffers for each phase, NB - 1 tiles in flight and one barrier per tile; each wave converts what it multiplies.
+template <int D> constexpr int kWideStage = 96 * 1024 * D / 128;
+template <int D, bool STEP>
+__global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
+  constexpr int KS = D / 16, DT = D / 32, RP = 128, CH = D / 4, NF = 2 * DT;     // NF: 1 KiB pieces of a tile, K then V
+  constexpr int DH = D / 2, LDO = DH + 4;               // the accumulators are merged in two halves of the columns
+  extern __shared__ __align__(16) char lds_raw[];
+  __shared__ int s_scan[24], s_flag, s_bad;
+  float* const s_o = (float*)lds_raw;                   // [8][32][LDO], on top of the tiles
+  float* const s_m = (float*)(lds_raw + kWideStage<D>); // [8][32]
+  float* const s_l = s_m + 8 * 32;
+  int* const s_start = (int*)(s_l + 8 * 32);            // [B + 1]
+  int* const s_row = s_start + B + 1;                   // [B + 1]
+  const int tid = threadIdx.x, G = Hq / Hkv, w_id = blockIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, ln = lane & 31, lg = lane >> 5;
+  Share sh = find_share<512, RP>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, merge_cost, s_start, s_row, s_scan, status);
+
+  auto run = [&](auto nqt_tag, const Unit& un) {
+    constexpr int NQT = decltype(nqt_tag)::value, NPH = 8 / NQT, LPW = NF / NQT;
+    constexpr int NB = kWideStage<D> / (NPH * NF * 1024);     // buffers: 3 or 6
+    const int32_t* __restrict__ bt = block_table + (size_t)seq_slot[un.b] * max_pages;
+    const int qt = wave % NQT, ph = wave / NQT;
+    const bool has_rows = qt * 32 < un.R;               // a wave without query rows only moves data
+    const int t_begin = 4 * un.s_lo, t_end = min(4 * un.s_hi, un.n_tiles);
+    const int n_it = (t_end - t_begin + NPH - 1) / NPH;
+    bool bad = false;
+    auto tile_of = [&](int i) { return min(t_begin + ph + NPH * i, un.n_tiles - 1); };   // a phase without a tile moves the last one again
+    auto page_of = [&](int t) {
+      const int page = bt[t * kTile / kPage];
+      if ((unsigned)page < (unsigned)n_pages) return page;
+      bad = true;
+      return 0;
+    };
+    const size_t head = (size_t)un.h * 2 * (kTile * D) + lane * 16;
+    auto request = [&](int t, int buf) {                // this wave's share of a tile: pieces qt, qt + NQT, ..
+      const size_t off = (size_t)page_of(t) * ((size_t)Hkv * kPage * D) + (size_t)(t & 1) * (kTile * D) + head;
+#pragma unroll
+      for (int j = 0; j < LPW; ++j) {
+        const int f = qt + NQT * j;
+        const bool is_k = NQT * (j + 1) <= DT ? true : NQT * j >= DT ? false : f < DT;
+        copy_to_lds((is_k ? k_pages : v_pages) + off + (is_k ? f : f - DT) * 1024, lds_raw + ((size_t)(buf * NPH + ph) * NF + f) * 1024);
+      }
+    };
+    const int qr = qt * 32 + ln;
+    const int lim = qr < un.R ? un.c + (un.qr0 + qr) / G : -1;
+    u32x4 qf[KS];
+    {
+      const int qc = un.qr0 + min(qr, un.R - 1);
+      const uint16_t* src = q + (size_t)(un.row0 + qc / G) * q_stride + (size_t)(un.h * G + qc % G) * D + lg * (D / 2);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) qf[s] = *(const u32x4*)(src + s * 8);
+    }
+    // the query loads in front and the requests unconditional, so that the wait for the queries leaves the requests in flight
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < NB - 1; ++i) request(tile_of(i), i);
+    __builtin_amdgcn_sched_barrier(0);
+    bool range = false;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) { asm volatile("" : "+v"(qf[s])); qf[s] = query8<STEP>(qf[s], range); }
+    f32x16 o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    int page = page_of(tile_of(0)), buf = 0;
+    float ks = k_scale[(size_t)page * Hkv + un.h], vs = v_scale[(size_t)page * Hkv + un.h];
+    for (int i = 0; i < n_it; ++i) {
+      // this wave's share of tile i has arrived (the up to NB - 2 requested behind it may be in flight), then everybody's; nobody reads tile i - 1 any more,
+      // whose buffer takes tile i + NB - 1.  The last tiles have NB - 1 requests of tiles behind the end in their place: the counts hold all the way.
+      wait_requests<(NB - 2) * LPW>();
+      __builtin_amdgcn_sched_barrier(0);
+      request(tile_of(i + NB - 1), buf == 0 ? NB - 1 : buf - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      const int t = t_begin + ph + NPH * i;
+      page = page_of(tile_of(i + 1));
+      const float ks1 = k_scale[(size_t)page * Hkv + un.h], vs1 = v_scale[(size_t)page * Hkv + un.h];
+      if (has_rows && t < t_end) {
+        const char* stage = lds_raw + (size_t)(buf * NPH + ph) * NF * 1024 + lane * 16;
+        u32x4 kc[DT], vc[DT];
+#pragma unroll
+        for (int s = 0; s < DT; ++s) kc[s] = *(const u32x4*)(stage + s * 1024);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 st;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st[r] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) st = mfma32(values8(kc[s / 2][2 * (s % 2)], kc[s / 2][2 * (s % 2) + 1], ks), as_f16x8(qf[s]), st);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < DT; ++s) vc[s] = *(const u32x4*)(stage + (DT + s) * 1024);
+        __builtin_amdgcn_sched_barrier(0);
+        f16x8 pf[2];
+        softmax_tile<DT>(st, (t + 1) * kTile - 1 <= un.c_all, t * kTile + 16 * lg, lim, scale_log2e, m_run, l_run, o, pf);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int t2 = 0; t2 < 2; ++t2) o[dt] = mfma32(values8(vc[dt][2 * t2], vc[dt][2 * t2 + 1], vs), pf[t2], o[dt]);
+      }
+      ks = ks1;
+      vs = vs1;
+      buf = buf == NB - 1 ? 0 : buf + 1;
+    }
+    if (bad && lane == 0) s_bad = 1;
+    if (range && status) atomicOr(status, BS_FAULT_RANGE);
+    wait_requests<0>();                                 // the tiles' buffers become the accumulators'
+
+    // ---- merge of the phases of every query tile, half of the columns at a time
+    const uint32_t part = partial_row<RP>(w_id, un.s_lo == 0);
+    const wt_buf bo = wt_buffer(part_o), bm = wt_buffer(part_ml);
+    const bool bad_unit = s_bad != 0;
+    if (bad_unit && tid == 0 && status) atomicOr(status, BS_FAULT_KV_PAGES);
+    l_run = sum_halves(l_run);
+    if (lg == 0) { s_m[wave * 32 + ln] = m_run; s_l[wave * 32 + ln] = l_run; }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (half) __syncthreads();
+      float* mine = s_o + (size_t)wave * 32 * LDO;
+#pragma unroll
+      for (int d2 = 0; d2 < DT / 2; ++d2)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const f32x16& a = o[half * (DT / 2) + d2];
+          *(f32x4*)(mine + ln * LDO + d2 * 32 + 8 * i4 + 4 * lg) = f32x4{a[4 * i4], a[4 * i4 + 1], a[4 * i4 + 2], a[4 * i4 + 3]};
+        }
+      __syncthreads();
+      for (int it = tid; it < un.R * (CH / 2); it += 512) {
+        const int r = it / (CH / 2), ch = it % (CH / 2), tq = r / 32, lr = r % 32;
+        float mw[NPH], mt = -INFINITY, lt = 0.f;
+#pragma unroll
+        for (int w = 0; w < NPH; ++w) { mw[w] = s_m[(w * NQT + tq) * 32 + lr]; mt = fmaxf(mt, mw[w]); }
+        f32x4 acc{0.f, 0.f, 0.f, 0.f};
+        if (mt != -INFINITY)
+#pragma unroll
+          for (int w = 0; w < NPH; ++w) {
+            const float f = __builtin_amdgcn_exp2f(mw[w] - mt);
+            lt += s_l[(w * NQT + tq) * 32 + lr] * f;
+            const f32x4 v = *(const f32x4*)(s_o + ((size_t)(w * NQT + tq) * 32 + lr) * LDO + ch * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += v[e] * f;
+          }
+        const int col = half * DH + ch * 4;
+        if (!un.whole) {
+          wt_store4(bo, ((part + r) * D + col) * 4, acc);
+          if (half == 0 && ch == 0) wt_store2(bm, (part + r) * 8, bad_unit ? INFINITY : mt, lt);
+        } else if (!bad_unit) {
+          const int rr = un.qr0 + r;
+          store4<D, STEP>(out, Hq, un.row0 + rr / G, (un.h * G + rr % G) * D + col, acc, 1.0f / lt, status);
+        }
+      }
+    }
+  };
+
+  while (sh.x < sh.x_end) {
+    const Unit un = find_unit<RP>(sh, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv);
+    if (tid == 0) s_bad = 0;
+    __syncthreads();                                    // LDS of the unit before is no longer read
+    if (un.R > 64) run(std::integral_constant<int, 4>{}, un);
+    else run(std::integral_constant<int, 2>{}, un);
+    if (!un.whole && publish_arrival(counters + un.w_first, un.w_last - un.w_first + 1, &s_flag)) merge_unit<512, RP, D, STEP>(un, part_o, part_ml, out, Hq, G, status);
+    sh.x = un.first + un.s_hi;
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // the next unit counts its own requests
+#endif
+    __syncthreads();
+  }
+}
+
+// Up to 32 rows for each KV head: four waves that share the tokens, two workgroups on a CU; more: eight waves, one workgroup.
+bool is_wide(int G, int q_max) { return (long long)q_max * G > 32; }
+int workgroups(bool wide) { return (wide ? 1 : 2) * kCUs; }
+size_t partial_floats(bool wide, int D) { return (size_t)2 * workgroups(wide) * (wide ? 128 : 32) * (D + 2); }
+
+template <int D, bool STEP>
 void launch(const KvqView& kv, const KvqSeqs& s, int Hq, const void* q, size_t q_stride, KvqOut out, int32_t* status, void* workspace, hipStream_t st) {
-  constexpr int RP = 32 * NQ;
-  const int grid = workgroups(NQ);
+  const bool wide = is_wide(Hq / kv.Hkv, s.n_max);
+  const int grid = workgroups(wide), RP = wide ? 128 : 32;
   float* part_ml = (float*)((char*)workspace + kCounters * sizeof(int32_t));
   float* part_o = part_ml + (size_t)2 * grid * RP * 2;
-  const size_t o = (size_t)4 * 32 * (D + 4) * 4, qb = (size_t)NQ * (D / 16) * 1024;
-  const size_t lds = (o > qb ? o : qb) + (size_t)2 * 4 * RP * 4 + (size_t)(s.B + 1) * 8;
-  auto kern = kvq_attention_kernel<NQ, D, STEP>;
-  static const hipError_t set = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 120 * 1024);
+  const size_t lists = (size_t)(s.B + 1) * 8;
+  const size_t lds = wide ? kWideStage<D> + 2 * 8 * 32 * 4 + lists : (size_t)4 * 32 * (D + 4) * 4 + 2 * 4 * 32 * 4 + lists;
+  auto kern = wide ? kvq_wide_kernel<D, STEP> : kvq_attention_kernel<1, D, STEP>;
+  static const hipError_t set[2] = {hipFuncSetAttribute((const void*)kvq_wide_kernel<D, STEP>, hipFuncAttributeMaxDynamicSharedMemorySize, 144 * 1024),
+                                    hipFuncSetAttribute((const void*)kvq_attention_kernel<1, D, STEP>, hipFuncAttributeMaxDynamicSharedMemorySize, 112 * 1024)};
   (void)set;
   const float scale_log2e = 1.4426950408889634f / sqrtf((float)D);
-  hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, st, s.slot, s.pos, s.n, s.n_add, s.n_max, s.B, kv.block_table, kv.n_slots, kv.max_pages, kv.n_pages, kv.k, kv.v,
-                     kv.ks, kv.vs, Hq, kv.Hkv, scale_log2e, (const uint16_t*)q, q_stride, out, 2, part_o, part_ml, (int32_t*)workspace, status);
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(wide ? 512 : 256), lds, st, s.slot, s.pos, s.n, s.n_add, s.n_max, s.B, kv.block_table, kv.n_slots, kv.max_pages, kv.n_pages,
+                     kv.k, kv.v, kv.ks, kv.vs, Hq, kv.Hkv, scale_log2e, (const uint16_t*)q, q_stride, out, 2, part_o, part_ml, (int32_t*)workspace, status);
 }
 }  // namespace
 
 size_t kvq_attention_workspace(int Hq, int Hkv, int D, int q_max) {
-  const int NQ = query_tiles(Hq / Hkv, q_max);
-  size_t most = 0;
-  for (int n = 1; n <= NQ; n *= 2) { const size_t b = (size_t)2 * workgroups(n) * 32 * n * (D + 2) * sizeof(float); most = b > most ? b : most; }
-  return kCounters * sizeof(int32_t) + most;
+  size_t most = partial_floats(false, D);
+  if (is_wide(Hq / Hkv, q_max) && partial_floats(true, D) > most) most = partial_floats(true, D);
+  return kCounters * sizeof(int32_t) + most * sizeof(float);
 }
 
 void launch_kvq_attention(const KvqView& kv, const KvqSeqs& s, int Hq, const void* qrows, size_t q_stride, void* out, int32_t* status, void* workspace, hipStream_t st) {
-  const int NQ = query_tiles(Hq / kv.Hkv, s.n_max);
   const KvqOut o{out, 0};
-#define BS_KVQ(NQ_, D_) launch<NQ_, D_, false>(kv, s, Hq, qrows, q_stride, o, status, workspace, st)
-  if (kv.D == 128) { if (NQ == 1) BS_KVQ(1, 128); else if (NQ == 2) BS_KVQ(2, 128); else BS_KVQ(4, 128); }
-  else { if (NQ == 1) BS_KVQ(1, 64); else if (NQ == 2) BS_KVQ(2, 64); else BS_KVQ(4, 64); }
-#undef BS_KVQ
+  if (kv.D == 128) launch<128, false>(kv, s, Hq, qrows, q_stride, o, status, workspace, st);
+  else launch<64, false>(kv, s, Hq, qrows, q_stride, o, status, workspace, st);
 }
