@@ -782,8 +782,8 @@ bs_status bs_kvq_attention(const bs_kvq_desc* kv, int B, const int32_t* seq_slot
   if (!kvq_heads_ok(n_q_heads, kv->n_kv_heads, kv->head_dim) || B < 1 || B > 4096 || q_max < 1 || (int64_t)q_max > (int64_t)kv->max_pages_per_seq * kPage ||
       q_stride < (int64_t)n_q_heads * kv->head_dim)
     return BS_ESHAPE;
-  // steps of 128 tokens over all units, counted in 32 bits
-  if ((int64_t)B * kv->n_kv_heads * (kv->max_pages_per_seq / 2 + 1) > ((int64_t)1 << 30) / ((int64_t)q_max * (n_q_heads / kv->n_kv_heads) / 128 + 1)) return BS_ESHAPE;
+  // 38 for each step of 128 tokens at most, over all units, counted in 32 bits
+  if ((int64_t)B * kv->n_kv_heads * (kv->max_pages_per_seq / 2 + 1) > ((int64_t)1 << 25) / ((int64_t)q_max * (n_q_heads / kv->n_kv_heads) / 128 + 1)) return BS_ESHAPE;
   if (workspace_bytes < kvq_attention_workspace(n_q_heads, kv->n_kv_heads, kv->head_dim, q_max)) return BS_ECAPACITY;
   const KvqSeqs s{B, q_max, 0, seq_slot, ctx_len, q_len, nullptr, 0, 0};
   launch_kvq_attention(view_of(*kv), s, n_q_heads, q, (size_t)q_stride, out, status, workspace, (hipStream_t)stream);

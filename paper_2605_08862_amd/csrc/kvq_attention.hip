@@ -1,13 +1,13 @@
 // Ragged causal attention over the 8-bit cache (codes, scales and element order: kvq.h).
 //
-// One launch and no work list.  A unit is (sequence, KV head, block of at most 32 NQ packed query rows); its K/V stream is cut into steps of 128 tokens, and
-// the steps of all units, in order, into equal shares, one per workgroup (a multiple of the CUs).  Every workgroup finds its share from a prefix sum over the
-// sequences that it makes itself.  A share can begin and end inside a unit: the workgroup then leaves a partial (rows, maximum, sum), and the last of a
-// unit's workgroups to arrive merges them (publish_arrival, common.h; nobody waits).
-//   * The four waves of a workgroup take a 32-token tile each of every step, with an online softmax of their own (attn_softmax.h), merged at a unit's end.
+// No work list.  A unit is (sequence, KV head, block of packed query rows); its K/V stream is cut into steps of 128 tokens, and the steps of all units, in a
+// row, into equal shares, one for each workgroup (a multiple of the CUs).  Every workgroup finds its share from a prefix sum over the sequences that it makes
+// itself.  A share can begin and end inside a unit: the workgroup then leaves a partial (rows, maximum, sum), and the last of a unit's workgroups to arrive
+// merges them, in groups of four or eight where there are many (publish_arrival, common.h; nobody waits).
+//   * Up to 32 rows of a unit: four waves take a 32-token tile each of every step, with an online softmax of their own (attn_softmax.h), merged at the unit's end.
+//     More: eight waves, kvq_wide_kernel.
 //   * S^T = K Q^T and O^T = V^T P^T on the 32 x 32 x 16 f16 MFMA.  A lane's sixteen bytes of codes are operands of two K-steps: one conversion with the block's
 //     scale gives two exact float16 values, so nothing is rounded that the 16-bit cache would not round.
-//   * Query fragments lie in LDS; K/V tiles are loaded two ahead into registers.
 #include "kvq.h"
 #include "attn_softmax.h"
 #include <type_traits>
@@ -15,7 +15,6 @@
 namespace {
 
 constexpr int kStep = 4 * kTile;                       // tokens of a step: a tile for each wave
-constexpr int kCounters = 1024;                        // one per workgroup, rounded up
 
 struct KvqOut { void* p; int ld; };                    // ld > 0: float16 rows in chunk order (act_index); 0: bf16 [rows][Hq][D]
 
@@ -38,23 +37,41 @@ __device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
 }
 
 // ---- the shares ------------------------------------------------------------------------------------------------------------------
-// Steps of the block of RP rows at qb of a sequence of n rows behind c tokens: of the tokens that its last row sees.
+// All units in a row (sequence, KV head, block) have a length: kUnitCost and step_cost for each of their steps, in units of 1/8 step of a launch that is bound
+// by memory.  The workgroups cut that into W equal parts; a cut is moved to the next step's start, and to the unit's end or start where less than kSnap + 1
+// steps would be left on that side.  So a share is a run of steps, and what a unit costs besides its steps (its queries, the merge of the waves) counts.
+constexpr int kUnitCost = 24, kSnap = 2;
+template <bool WIDE> __device__ __forceinline__ int step_cost(int R) { return WIDE && R > 64 ? 14 : 8; }
+template <bool WIDE> constexpr int kBlock = WIDE ? 128 : 32;          // rows of a block
+// Steps of the block qb of a sequence of n rows behind c tokens: of the tokens that its last row sees.
 template <int RP> __device__ __forceinline__ int block_steps(int c, int n, int G, int qb) { return (c + min(n - 1, ((qb + 1) * RP - 1) / G) + kStep) / kStep; }
 
-struct Share { int x, x_end, size, b; };               // steps [x, x_end) of all, the length of a share, the sequence of step x
+struct Shares {
+  int total, W;                                         // length of everything, workgroups that have a share
+  unsigned long long per;                               // length of a share, 16 bits of fraction
+  float inv;                                            // its reciprocal
+  __device__ __forceinline__ int bound(int w) const { return w >= W ? total : (int)((w * per) >> 16); }
+  // the largest w with bound(w) <= p
+  __device__ __forceinline__ int of(int p) const {
+    int w = min(W - 1, (int)((float)p * inv));
+    while (w > 0 && bound(w) > p) --w;
+    while (w + 1 < W && bound(w + 1) <= p) ++w;
+    return w;
+  }
+};
 
-// Called by all threads.  s_start, s_row [B + 1]: first step and first packed row of every sequence; s_scan: 3 words for each wave.
-// A share is no shorter than sqrt(steps of the longest unit * merge_cost / 16), since its partials have to be merged by one workgroup.
-template <int THREADS, int RP>
-__device__ __forceinline__ Share find_share(const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
-                                            int n_max, int B, int n_slots, int max_pages, int G, int Hkv, int merge_cost, int* s_start, int* s_row, int* s_scan,
-                                            int32_t* __restrict__ status) {
-  constexpr int W = THREADS / 64;
+// Called by all threads.  s_start, s_row [B + 1]: where every sequence begins, and its first packed row; s_scan: 2 words for each wave.
+// A share is no shorter than `least`, and longer than a step, so that every share between two others of a unit has a step of it.
+template <int THREADS, bool WIDE>
+__device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
+                                              int n_max, int B, int n_slots, int max_pages, int G, int Hkv, int least, int* s_start, int* s_row, int* s_scan,
+                                              int32_t* __restrict__ status) {
+  constexpr int NW = THREADS / 64, RP = kBlock<WIDE>;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (B + THREADS - 1) / THREADS, lo = min(tid * per, B), hi = min(lo + per, B);
-  int steps = 0, rows = 0, fault = 0, most = 0;
+  int cost = 0, rows = 0, fault = 0;
   for (int b = lo; b < hi; ++b) {
-    s_start[b] = steps;
+    s_start[b] = cost;
     s_row[b] = rows;
     const int n = seq_n[b] + n_add, slot = seq_slot[b], c = seq_pos[b];
     if (n < 0 || n > n_max) { fault |= BS_FAULT_DRAFT_LEN; continue; }
@@ -64,75 +81,133 @@ __device__ __forceinline__ Share find_share(const int32_t* __restrict__ seq_slot
     if (c < 0 || (long long)c + n > (long long)max_pages * kPage) { fault |= BS_FAULT_KV_PAGES; continue; }
     const int blocks = (n * G + RP - 1) / RP;
     int s = 0;
-    for (int qb = 0; qb < blocks; ++qb) s += block_steps<RP>(c, n, G, qb);
-    most = max(most, block_steps<RP>(c, n, G, blocks - 1));
-    steps += s * Hkv;
+    for (int qb = 0; qb < blocks; ++qb) s += kUnitCost + step_cost<WIDE>(n * G - qb * RP) * block_steps<RP>(c, n, G, qb);
+    cost += s * Hkv;
   }
   if (fault && blockIdx.x == 0 && status) atomicOr(status, fault);
-  int is = steps, ir = rows;                            // exclusive prefix over the threads
+  int is = cost, ir = rows;                             // exclusive prefix over the threads
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int a = __shfl_up(is, o), r = __shfl_up(ir, o);
     if (lane >= o) { is += a; ir += r; }
-    most = max(most, __shfl_xor(most, o));
   }
-  if (lane == 63) { s_scan[wave] = is; s_scan[W + wave] = ir; s_scan[2 * W + wave] = most; }
+  if (lane == 63) { s_scan[wave] = is; s_scan[NW + wave] = ir; }
   __syncthreads();
-  int bs = is - steps, br = ir - rows, total = 0;
-  most = 0;
+  int bs = is - cost, br = ir - rows, total = 0;
 #pragma unroll
-  for (int w = 0; w < W; ++w) {
-    if (w < wave) { bs += s_scan[w]; br += s_scan[W + w]; }
+  for (int w = 0; w < NW; ++w) {
+    if (w < wave) { bs += s_scan[w]; br += s_scan[NW + w]; }
     total += s_scan[w];
-    most = max(most, s_scan[2 * W + w]);
   }
   for (int b = lo; b < hi; ++b) { s_start[b] += bs; s_row[b] += br; }
   if (tid == 0) s_start[B] = total;
   __syncthreads();
-  total = __builtin_amdgcn_readfirstlane(total);
-  int size = max((total + (int)gridDim.x - 1) / (int)gridDim.x, (int)sqrtf((float)most * (float)merge_cost * 0.0625f));
-  size = __builtin_amdgcn_readfirstlane(max(size, 1));
-  Share sh{(int)blockIdx.x * size, 0, size, 0};
-  sh.x_end = min(sh.x + size, total);
-  int top = B;                                          // largest b with s_start[b] <= x (sequences without steps are passed over)
-  while (top - sh.b > 1) { const int mid = (sh.b + top) >> 1; if (s_start[mid] <= sh.x) sh.b = mid; else top = mid; }
+  Shares sh;
+  sh.total = __builtin_amdgcn_readfirstlane(total);
+  sh.W = __builtin_amdgcn_readfirstlane(min((int)gridDim.x, max(1, total / least)));
+  sh.per = ((unsigned long long)sh.total << 16) / (unsigned)sh.W;
+  sh.inv = (float)sh.W / (float)max(sh.total, 1);
   return sh;
 }
 
-// The unit that step x of a share lies in, and the part [s_lo, s_hi) of its steps that the share has.
 struct Unit {
-  int b, h, n, c, row0;                                 // sequence, KV head, its rows, the tokens before them, first packed row
-  int first, steps, s_lo, s_hi;                         // first step of the unit among all
-  int qr0, R, n_tiles, c_all;                           // first row (query row x head) of the block in the sequence, rows, tiles, last position that every row sees
-  bool whole;
-  int w_first, w_last;                                  // workgroups that have a part
+  int b, h, qb, blocks;                                 // sequence, KV head, block of its blocks
+  int n, c, row0;                                       // rows of the sequence, tokens before them, first packed row
+  int first, steps, step;                               // where the unit begins, its steps, what one costs
+  __device__ __forceinline__ int end() const { return first + kUnitCost + step * steps; }
+  // step at which a cut at p is made
+  __device__ __forceinline__ int cut(int p) const {
+    const int j = (p - first - kUnitCost + step - 1) / step;
+    return p >= end() ? steps : p <= first + kUnitCost + kSnap * step ? 0 : steps - j <= kSnap ? steps : j;
+  }
+  // the first and the last workgroup that have steps of the unit
+  __device__ __forceinline__ int first_share(const Shares& sh) const { return sh.of(min(first + kUnitCost + kSnap * step, sh.total - 1)); }
+  __device__ __forceinline__ int last_share(const Shares& sh) const { return sh.of(first + kUnitCost + max(step * (steps - kSnap - 1), kSnap * step)); }
 };
-template <int RP>
-__device__ __forceinline__ Unit find_unit(Share& sh, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
-                                          int G, int Hkv) {
-  while (s_start[sh.b + 1] <= sh.x) ++sh.b;
-  Unit u;
-  u.b = sh.b = __builtin_amdgcn_readfirstlane(sh.b);
+template <bool WIDE>
+__device__ __forceinline__ void fill_unit(Unit& u, int G) {
+  constexpr int RP = kBlock<WIDE>;
+  u.steps = block_steps<RP>(u.c, u.n, G, u.qb);
+  u.step = step_cost<WIDE>(u.n * G - u.qb * RP);
+}
+template <bool WIDE>
+__device__ __forceinline__ void enter_sequence(Unit& u, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add, int G) {
+  u.b = __builtin_amdgcn_readfirstlane(u.b);
   u.n = seq_n[u.b] + n_add;
   u.c = seq_pos[u.b];
   u.row0 = __builtin_amdgcn_readfirstlane(s_row[u.b]);
-  const int first = __builtin_amdgcn_readfirstlane(s_start[u.b]);
-  const int per_head = __builtin_amdgcn_readfirstlane((s_start[u.b + 1] - first) / Hkv);
-  u.h = (sh.x - first) / per_head;
-  u.first = first + u.h * per_head;
-  int qb = 0;
-  for (int s; u.first + (s = block_steps<RP>(u.c, u.n, G, qb)) <= sh.x; ++qb) u.first += s;
-  u.steps = block_steps<RP>(u.c, u.n, G, qb);
-  u.s_lo = sh.x - u.first;
-  u.s_hi = min(u.steps, sh.x_end - u.first);
-  u.qr0 = qb * RP;
-  u.R = min(u.n * G - u.qr0, RP);
-  u.n_tiles = (u.c + min(u.n - 1, (u.qr0 + RP - 1) / G)) / kTile + 1;
-  u.c_all = u.c + u.qr0 / G;
-  u.whole = u.s_lo == 0 && u.s_hi == u.steps;
-  u.w_first = u.first / sh.size;
-  u.w_last = (u.first + u.steps - 1) / sh.size;
+  u.first = __builtin_amdgcn_readfirstlane(s_start[u.b]);
+  u.blocks = (u.n * G + kBlock<WIDE> - 1) / kBlock<WIDE>;
+  u.h = u.qb = 0;
+  fill_unit<WIDE>(u, G);
+}
+// The unit that p (below the total) lies in.
+template <bool WIDE>
+__device__ __forceinline__ Unit unit_at(int p, int B, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
+                                        int G, int Hkv) {
+  Unit u;
+  int lo = 0, hi = B;                                   // largest b with s_start[b] <= p (sequences without units are passed over)
+  while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_start[mid] <= p) lo = mid; else hi = mid; }
+  u.b = lo;
+  enter_sequence<WIDE>(u, s_start, s_row, seq_pos, seq_n, n_add, G);
+  const int head = __builtin_amdgcn_readfirstlane((s_start[u.b + 1] - u.first) / Hkv);
+  u.h = (p - u.first) / head;
+  u.first += u.h * head;
+  while (u.end() <= p) { u.first = u.end(); ++u.qb; fill_unit<WIDE>(u, G); }
   return u;
+}
+// The unit behind; false behind the last one.
+template <bool WIDE>
+__device__ __forceinline__ bool next_unit(Unit& u, int B, int Hkv, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n,
+                                          int n_add, int G) {
+  u.first = u.end();
+  if (++u.qb < u.blocks) { fill_unit<WIDE>(u, G); return true; }
+  u.qb = 0;
+  if (++u.h < Hkv) { fill_unit<WIDE>(u, G); return true; }
+  do { if (++u.b >= B) return false; } while (s_start[u.b + 1] == s_start[u.b]);
+  enter_sequence<WIDE>(u, s_start, s_row, seq_pos, seq_n, n_add, G);
+  return true;
+}
+// What a workgroup does of a unit.
+struct Part {
+  int b, h, row0, qr0, R, c, s_lo, s_hi, n_tiles, c_all;   // qr0: first row (query row x head) of the block in the sequence; c_all: last position that every row sees
+  int w_first, w_last;                                     // workgroups that have a part
+  bool whole;
+};
+template <bool WIDE>
+__device__ __forceinline__ Part part_of(const Unit& u, const Shares& sh, int s_lo, int s_hi, int G) {
+  constexpr int RP = kBlock<WIDE>;
+  Part t;
+  t.b = u.b; t.h = u.h; t.row0 = u.row0; t.c = u.c;
+  t.qr0 = u.qb * RP;
+  t.R = min(u.n * G - t.qr0, RP);
+  t.s_lo = s_lo; t.s_hi = s_hi;
+  t.n_tiles = (u.c + min(u.n - 1, (t.qr0 + RP - 1) / G)) / kTile + 1;
+  t.c_all = u.c + t.qr0 / G;
+  t.whole = s_lo == 0 && s_hi == u.steps;
+  t.w_first = t.w_last = blockIdx.x;
+  if (!t.whole) {
+    t.w_first = __builtin_amdgcn_readfirstlane(s_lo == 0 ? (int)blockIdx.x : u.first_share(sh));
+    t.w_last = __builtin_amdgcn_readfirstlane(s_hi == u.steps ? (int)blockIdx.x : u.last_share(sh));
+  }
+  return t;
+}
+// Calls f(part) for every part of this workgroup's share.
+template <bool WIDE, typename F>
+__device__ __forceinline__ void for_parts(const Shares& sh, int B, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n,
+                                          int n_add, int G, int Hkv, const F& f) {
+  const int w = blockIdx.x;
+  if (w >= sh.W || sh.total == 0) return;
+  const int p0 = __builtin_amdgcn_readfirstlane(sh.bound(w)), p1 = __builtin_amdgcn_readfirstlane(sh.bound(w + 1));
+  Unit u = unit_at<WIDE>(p0, B, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv);
+  int s_lo = u.cut(p0);
+  while (true) {
+    const bool last = u.end() >= p1;
+    const int s_hi = last ? u.cut(p1) : u.steps;
+    if (s_lo < s_hi) f(part_of<WIDE>(u, sh, s_lo, s_hi, G));
+    s_lo = 0;
+    if (last || !next_unit<WIDE>(u, B, Hkv, s_start, s_row, seq_pos, seq_n, n_add, G)) break;
+  }
 }
 // Partial rows: two places for each workgroup, for a unit that began before its share and for one that goes on behind it.
 template <int RP> __device__ __forceinline__ uint32_t partial_row(int w, bool began_here) { return (uint32_t)(2 * w + (began_here ? 1 : 0)) * RP; }
@@ -147,45 +222,100 @@ __device__ __forceinline__ void store4(const KvqOut& out, int Hq, int row, int c
   }
 }
 
-// Merges the partials of a unit; called by the last of its workgroups to arrive.  An item is four columns of a row, eight partials in flight.
-template <int THREADS, int RP, int D, bool STEP>
-__device__ __forceinline__ void merge_unit(const Unit& un, const float* part_o, const float* part_ml, const KvqOut& out, int Hq, int G, int32_t* status) {
-  constexpr int CH = D / 4, GC = 8;
-  const wt_buf bo = wt_buffer(part_o), bm = wt_buffer(part_ml);
-  for (int it = threadIdx.x; it < un.R * CH; it += THREADS) {
-    const int r = it / CH, ch = it % CH;
-    float m = -INFINITY, l = 0.f;
-    f32x4 acc{0.f, 0.f, 0.f, 0.f};
-    for (int c0 = un.w_first; c0 <= un.w_last; c0 += GC) {
-      wt_f32x2 ml[GC];
-      f32x4 v[GC];
+// ---- merge of a unit's parts -------------------------------------------------------------------------------------------------------
+// Partial rows: part_o [2 W][RP][D], and (maximum, sum) part_ml [kLevels][2 W][RP][2].  Parts are merged in groups of F neighbours by the last of a group to
+// arrive, into the place of the group's first part, the merged parts again, and so on: a unit of 64 parts of 119 rows is 4 MB, which one workgroup alone read in
+// 70 us of a launch of 88.  Maxima and sums of a level have a place of their own, since several threads read those of a row.
+// counters [kLevels][kMaxShares], zero between launches; a workgroup is the first of at most one group of more than one part on every level.
+constexpr int kLevels = 5, kMaxShares = 2 * kCUs;
+struct Parts { float *o, *ml; int32_t* counters; };
+template <int RP> constexpr uint32_t kMlLevel = (uint32_t)2 * kMaxShares * RP;      // rows of a level
+
+// Merges `count` parts, `stride` apart from part i0 of the unit on, on level `level`.  An item is four columns of a row; the loads of NI items and GC parts are in
+// flight together.
+template <int THREADS, int RP, int D, bool STEP, int NI, int GC>
+__device__ __forceinline__ void merge_group(const Part& un, const Parts& p, int level, int i0, int stride, int count, bool last, const KvqOut& out, int Hq, int G,
+                                            int32_t* status) {
+  constexpr int CH = D / 4;
+  const wt_buf bo = wt_buffer(p.o), bm = wt_buffer(p.ml);
+  const int items = un.R * CH;
+  const uint32_t to = partial_row<RP>(un.w_first + i0, i0 == 0);
+  for (int it0 = threadIdx.x; it0 < items; it0 += THREADS * NI) {
+    float m[NI], l[NI];
+    f32x4 acc[NI];
+#pragma unroll
+    for (int k = 0; k < NI; ++k) { m[k] = -INFINITY; l[k] = 0.f; acc[k] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+    for (int c0 = 0; c0 < count; c0 += GC) {
+      wt_f32x2 ml[GC][NI];
+      f32x4 v[GC][NI];
 #pragma unroll
       for (int u = 0; u < GC; ++u) {
-        const int c = min(c0 + u, un.w_last);
-        const uint32_t pr = partial_row<RP>(c, c == un.w_first) + r;
-        ml[u] = wt_load2(bm, pr * 8);
-        v[u] = wt_load4(bo, (pr * D + ch * 4) * 4);
+        const int i = i0 + min(c0 + u, count - 1) * stride;
+        const uint32_t row = partial_row<RP>(un.w_first + i, i == 0);
+#pragma unroll
+        for (int k = 0; k < NI; ++k) {                  // (an item behind the last one: the last one)
+          const int it = min(it0 + k * THREADS, items - 1);
+          ml[u][k] = wt_load2(bm, (level * kMlLevel<RP> + row + it / CH) * 8);
+          v[u][k] = wt_load4(bo, ((row + it / CH) * D + it % CH * 4) * 4);
+        }
       }
-      float mg = m;
 #pragma unroll
-      for (int u = 0; u < GC; ++u) mg = fmaxf(mg, ml[u][0]);
-      if (mg == -INFINITY) continue;
-      const float f0 = __builtin_amdgcn_exp2f(m - mg);
-      l *= f0;
+      for (int k = 0; k < NI; ++k) {
+        float mg = m[k];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] *= f0;
+        for (int u = 0; u < GC; ++u) { if (c0 + u >= count) ml[u][k] = wt_f32x2{-INFINITY, 0.f}; mg = fmaxf(mg, ml[u][k][0]); }
+        if (mg == -INFINITY) continue;
+        const float f0 = __builtin_amdgcn_exp2f(m[k] - mg);
+        l[k] *= f0;
 #pragma unroll
-      for (int u = 0; u < GC; ++u) {
-        const float f = c0 + u <= un.w_last ? __builtin_amdgcn_exp2f(ml[u][0] - mg) : 0.f;
-        l += ml[u][1] * f;
+        for (int e = 0; e < 4; ++e) acc[k][e] *= f0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += v[u][e] * f;
+        for (int u = 0; u < GC; ++u) {
+          const float f = __builtin_amdgcn_exp2f(ml[u][k][0] - mg);
+          l[k] += ml[u][k][1] * f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[k][e] += v[u][k][e] * f;
+        }
+        m[k] = mg;
       }
-      m = mg;
     }
-    if (m == INFINITY) continue;                        // a bad page: the row stays as it is
-    const int qr = un.qr0 + r;
-    store4<D, STEP>(out, Hq, un.row0 + qr / G, (un.h * G + qr % G) * D + ch * 4, acc, 1.0f / l, status);
+#pragma unroll
+    for (int k = 0; k < NI; ++k) {
+      const int it = it0 + k * THREADS;
+      if (it >= items) continue;
+      const int r = it / CH, ch = it % CH;
+      if (!last) {
+        wt_store4(bo, ((to + r) * D + ch * 4) * 4, acc[k]);
+        if (ch == 0) wt_store2(bm, ((level + 1) * kMlLevel<RP> + to + r) * 8, m[k], l[k]);
+      } else if (m[k] != INFINITY) {                    // (infinite: a bad page, the row stays as it is)
+        const int qr = un.qr0 + r;
+        store4<D, STEP>(out, Hq, un.row0 + qr / G, (un.h * G + qr % G) * D + ch * 4, acc[k], 1.0f / l[k], status);
+      }
+    }
+  }
+}
+// Called by all threads of a workgroup that has stored its part of a cut unit on level 0.
+template <int THREADS, int RP, int D, bool STEP>
+__device__ __forceinline__ void merge_unit(const Part& un, const Parts& p, const KvqOut& out, int Hq, int G, int32_t* status, int* s_flag) {
+  const bool few = un.R * (D / 4) <= THREADS;           // few rows, as of one long sequence
+  const int F = few ? 8 : 4, n = un.w_last - un.w_first + 1;
+  int i = (int)blockIdx.x - un.w_first;
+  for (int level = 0, stride = 1; stride < n; ++level, stride *= F) {
+    i -= i % (stride * F);
+    const int count = min(F, (n - i + stride - 1) / stride);
+    const bool last = stride * F >= n;
+    if (count > 1) {
+      if (!publish_arrival(p.counters + level * kMaxShares + un.w_first + i, count, s_flag)) return;
+      if (few) merge_group<THREADS, RP, D, STEP, 1, 8>(un, p, level, i, stride, count, last, out, Hq, G, status);
+      else merge_group<THREADS, RP, D, STEP, 4, 4>(un, p, level, i, stride, count, last, out, Hq, G, status);
+    } else {                                            // nothing to merge with on this level
+      const wt_buf bm = wt_buffer(p.ml);
+      const uint32_t row = partial_row<RP>(un.w_first + i, i == 0);
+      for (int r = threadIdx.x; r < un.R; r += THREADS) {
+        const wt_f32x2 ml = wt_load2(bm, (level * kMlLevel<RP> + row + r) * 8);
+        wt_store2(bm, ((level + 1) * kMlLevel<RP> + row + r) * 8, ml[0], ml[1]);
+      }
+    }
   }
 }
 
@@ -193,8 +323,13 @@ __device__ __forceinline__ void merge_unit(const Unit& un, const float* part_o, 
 template <int DT>
 __device__ __forceinline__ void softmax_tile(const f32x16& st, bool full, int tok0, int lim, float scale_log2e, float& m_run, float& l_run, f32x16 (&o)[DT], f16x8 (&pf)[2]) {
   float y[16];
+  if (full) {                                           // the same for the wave
 #pragma unroll
-  for (int i = 0; i < 16; ++i) y[i] = full || tok0 + i <= lim ? st[i] : -INFINITY;
+    for (int i = 0; i < 16; ++i) y[i] = st[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = tok0 + i <= lim ? st[i] : -INFINITY;
+  }
   float mloc = y[0];
 #pragma unroll
   for (int i = 1; i < 16; ++i) mloc = fmaxf(mloc, y[i]);
@@ -224,22 +359,24 @@ __device__ __forceinline__ void softmax_tile(const f32x16& st, bool full, int to
 // Sixteen bytes of a query row as float16.
 template <bool STEP> __device__ __forceinline__ u32x4 query8(u32x4 v, bool& range) {
   if constexpr (STEP) return v;
-  const bf16x8 y = __builtin_bit_cast(bf16x8, v);
-  f16x8 z;
+  float y[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float f = (float)y[e];
-    if (!(fabsf(f) <= 65504.f)) { f = f16_saturate(f); range = true; }
-    z[e] = (f16)f;
+  for (int e = 0; e < 4; ++e) { y[2 * e] = __uint_as_float(v[e] << 16); y[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u); }
+  f16x4 lo = f16x4{(f16)y[0], (f16)y[1], (f16)y[2], (f16)y[3]}, hi = f16x4{(f16)y[4], (f16)y[5], (f16)y[6], (f16)y[7]};
+  if (f16x4_out_of_range(lo) || f16x4_out_of_range(hi)) {
+    range = true;
+    lo = f16x4{(f16)f16_saturate(y[0]), (f16)f16_saturate(y[1]), (f16)f16_saturate(y[2]), (f16)f16_saturate(y[3])};
+    hi = f16x4{(f16)f16_saturate(y[4]), (f16)f16_saturate(y[5]), (f16)f16_saturate(y[6]), (f16)f16_saturate(y[7])};
   }
-  return __builtin_bit_cast(u32x4, z);
+  const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
+  return u32x4{a[0], a[1], b[0], b[1]};
 }
 
 #define BS_KVQ_PARAMS                                                                                                                                     \
   const int32_t *__restrict__ seq_slot, const int32_t *__restrict__ seq_pos, const int32_t *__restrict__ seq_n, int n_add, int n_max, int B,                \
       const int32_t *__restrict__ block_table, int n_slots, int max_pages, int n_pages, const uint8_t *__restrict__ k_pages, const uint8_t *__restrict__ v_pages, \
       const float *__restrict__ k_scale, const float *__restrict__ v_scale, int Hq, int Hkv, float scale_log2e, const uint16_t *__restrict__ q, size_t q_stride, \
-      KvqOut out, int merge_cost, float *__restrict__ part_o, float *__restrict__ part_ml, int32_t *__restrict__ counters, int32_t *__restrict__ status
+      KvqOut out, int least, Parts parts, int32_t *__restrict__ status
 
 // Blocks of up to 32 NQ rows, four waves.  STEP: inside bs_verify_step (float16 queries, output in chunk order).
 template <int NQ, int D, bool STEP>
@@ -247,7 +384,7 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) kvq_attention_kernel(BS_
   constexpr int KS = D / 16, DT = D / 32, RP = 32 * NQ, CH = D / 4;
   constexpr int LDO = D + 4;                            // row stride (floats) of an accumulator in LDS
   extern __shared__ __align__(16) char lds_raw[];
-  __shared__ int s_scan[12], s_flag;
+  __shared__ int s_scan[8], s_flag;
   u32x4* const s_q = (u32x4*)lds_raw;                   // [NQ][KS][64] query fragments; behind a unit's last product, the waves' accumulators
   float* const s_o = (float*)lds_raw;                   // [4][32][LDO]
   constexpr size_t kOBytes = (size_t)4 * 32 * LDO * 4, kQBytes = (size_t)NQ * KS * 1024;
@@ -257,9 +394,8 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) kvq_attention_kernel(BS_
   int* const s_row = s_start + B + 1;                   // [B + 1]
   const int tid = threadIdx.x, G = Hq / Hkv, w_id = blockIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, ln = lane & 31, lg = lane >> 5;
-  Share sh = find_share<256, RP>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, merge_cost, s_start, s_row, s_scan, status);
-  while (sh.x < sh.x_end) {
-    const Unit un = find_unit<RP>(sh, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv);
+  const Shares sh = find_shares<256, false>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, least, s_start, s_row, s_scan, status);
+  for_parts<false>(sh, B, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv, [&](const Part& un) {
     const int32_t* __restrict__ bt = block_table + (size_t)seq_slot[un.b] * max_pages;
     const int t0 = 4 * un.s_lo + wave, t_end = min(4 * un.s_hi, un.n_tiles);
     const int n_my = t0 < t_end ? (t_end - t0 + 3) / 4 : 0, t_last = t0 + (n_my - 1) * 4;
@@ -361,8 +497,8 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) kvq_attention_kernel(BS_
     }
 
     // ---- merge of the waves, one query tile at a time
-    const uint32_t part = partial_row<RP>(w_id, un.s_lo == 0);
-    const wt_buf bo = wt_buffer(part_o), bm = wt_buffer(part_ml);
+    const uint32_t part = partial_row<RP>(w_id, w_id == un.w_first);
+    const wt_buf bo = wt_buffer(parts.o), bm = wt_buffer(parts.ml);
     if (bad && lane == 0 && status) atomicOr(status, BS_FAULT_KV_PAGES);
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
@@ -404,10 +540,9 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) kvq_attention_kernel(BS_
         }
       }
     }
-    if (!un.whole && publish_arrival(counters + un.w_first, un.w_last - un.w_first + 1, &s_flag)) merge_unit<256, RP, D, STEP>(un, part_o, part_ml, out, Hq, G, status);
-    sh.x = un.first + un.s_hi;
+    if (!un.whole) merge_unit<256, RP, D, STEP>(un, parts, out, Hq, G, status, &s_flag);
     __syncthreads();                                    // LDS is the next unit's
-  }
+  });
 }
 
 // Waits until at most N of this wave's requests are in flight (and for its LDS accesses), then for the other waves.
@@ -432,7 +567,7 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
   constexpr int KS = D / 16, DT = D / 32, RP = 128, CH = D / 4, NF = 2 * DT;     // NF: 1 KiB pieces of a tile, K then V
   constexpr int DH = D / 2, LDO = DH + 4;               // the accumulators are merged in two halves of the columns
   extern __shared__ __align__(16) char lds_raw[];
-  __shared__ int s_scan[24], s_flag, s_bad;
+  __shared__ int s_scan[16], s_bad, s_flag;
   float* const s_o = (float*)lds_raw;                   // [8][32][LDO], on top of the tiles
   float* const s_m = (float*)(lds_raw + kWideStage<D>); // [8][32]
   float* const s_l = s_m + 8 * 32;
@@ -440,9 +575,9 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
   int* const s_row = s_start + B + 1;                   // [B + 1]
   const int tid = threadIdx.x, G = Hq / Hkv, w_id = blockIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, ln = lane & 31, lg = lane >> 5;
-  Share sh = find_share<512, RP>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, merge_cost, s_start, s_row, s_scan, status);
+  const Shares sh = find_shares<512, true>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, least, s_start, s_row, s_scan, status);
 
-  auto run = [&](auto nqt_tag, const Unit& un) {
+  auto run = [&](auto nqt_tag, const Part& un) {
     constexpr int NQT = decltype(nqt_tag)::value, NPH = 8 / NQT, LPW = NF / NQT;
     constexpr int NB = kWideStage<D> / (NPH * NF * 1024);     // buffers: 3 or 6
     const int32_t* __restrict__ bt = block_table + (size_t)seq_slot[un.b] * max_pages;
@@ -534,8 +669,8 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
     wait_requests<0>();                                 // the tiles' buffers become the accumulators'
 
     // ---- merge of the phases of every query tile, half of the columns at a time
-    const uint32_t part = partial_row<RP>(w_id, un.s_lo == 0);
-    const wt_buf bo = wt_buffer(part_o), bm = wt_buffer(part_ml);
+    const uint32_t part = partial_row<RP>(w_id, w_id == un.w_first);
+    const wt_buf bo = wt_buffer(parts.o), bm = wt_buffer(parts.ml);
     const bool bad_unit = s_bad != 0;
     if (bad_unit && tid == 0 && status) atomicOr(status, BS_FAULT_KV_PAGES);
     l_run = sum_halves(l_run);
@@ -579,32 +714,37 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
     }
   };
 
-  while (sh.x < sh.x_end) {
-    const Unit un = find_unit<RP>(sh, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv);
+  for_parts<true>(sh, B, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv, [&](const Part& un) {
     if (tid == 0) s_bad = 0;
     __syncthreads();                                    // LDS of the unit before is no longer read
     if (un.R > 64) run(std::integral_constant<int, 4>{}, un);
     else run(std::integral_constant<int, 2>{}, un);
-    if (!un.whole && publish_arrival(counters + un.w_first, un.w_last - un.w_first + 1, &s_flag)) merge_unit<512, RP, D, STEP>(un, part_o, part_ml, out, Hq, G, status);
-    sh.x = un.first + un.s_hi;
+    if (!un.whole) merge_unit<512, RP, D, STEP>(un, parts, out, Hq, G, status, &s_flag);
 #if defined(__HIP_DEVICE_COMPILE__)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // the next unit counts its own requests
 #endif
     __syncthreads();
-  }
+  });
 }
 
-// Up to 32 rows for each KV head: four waves that share the tokens, two workgroups on a CU; more: eight waves, one workgroup.
+// Blocks of 32 rows on four waves, two workgroups on a CU, or of up to 128 rows on eight waves.  The second reads K/V once for four times the rows, but has
+// more to do before and behind its steps, so it needs many units: 7B heads, 17 rows, 32 units of 20000 tokens 68 us on the first and 75 on the second, 64 of
+// 8000 93 and 64; 1.5B heads, 9 rows, 32 units of 8000 27 and 32; 7B heads, 9 rows, 128 of 8192 94 and 70.
 bool is_wide(int G, int q_max) { return (long long)q_max * G > 32; }
+bool runs_wide(const KvqSeqs& s, int G, int Hkv) { return is_wide(G, s.n_max) && s.B * Hkv > 32; }
 int workgroups(bool wide) { return (wide ? 1 : 2) * kCUs; }
-size_t partial_floats(bool wide, int D) { return (size_t)2 * workgroups(wide) * (wide ? 128 : 32) * (D + 2); }
+size_t workspace_bytes(bool wide, int D) {
+  const size_t rows = (size_t)2 * (wide ? 128 : 32);
+  return kLevels * kMaxShares * sizeof(int32_t) + rows * sizeof(float) * (kLevels * kMaxShares * 2 + (size_t)workgroups(wide) * D);
+}
 
 template <int D, bool STEP>
 void launch(const KvqView& kv, const KvqSeqs& s, int Hq, const void* q, size_t q_stride, KvqOut out, int32_t* status, void* workspace, hipStream_t st) {
-  const bool wide = is_wide(Hq / kv.Hkv, s.n_max);
+  const bool wide = runs_wide(s, Hq / kv.Hkv, kv.Hkv);
   const int grid = workgroups(wide), RP = wide ? 128 : 32;
-  float* part_ml = (float*)((char*)workspace + kCounters * sizeof(int32_t));
-  float* part_o = part_ml + (size_t)2 * grid * RP * 2;
+  int32_t* counters = (int32_t*)workspace;
+  float* ml = (float*)(counters + kLevels * kMaxShares);
+  const Parts parts{ml + (size_t)kLevels * 2 * kMaxShares * RP * 2, ml, counters};
   const size_t lists = (size_t)(s.B + 1) * 8;
   const size_t lds = wide ? kWideStage<D> + 2 * 8 * 32 * 4 + lists : (size_t)4 * 32 * (D + 4) * 4 + 2 * 4 * 32 * 4 + lists;
   auto kern = wide ? kvq_wide_kernel<D, STEP> : kvq_attention_kernel<1, D, STEP>;
@@ -613,14 +753,13 @@ void launch(const KvqView& kv, const KvqSeqs& s, int Hq, const void* q, size_t q
   (void)set;
   const float scale_log2e = 1.4426950408889634f / sqrtf((float)D);
   hipLaunchKernelGGL(kern, dim3(grid), dim3(wide ? 512 : 256), lds, st, s.slot, s.pos, s.n, s.n_add, s.n_max, s.B, kv.block_table, kv.n_slots, kv.max_pages, kv.n_pages,
-                     kv.k, kv.v, kv.ks, kv.vs, Hq, kv.Hkv, scale_log2e, (const uint16_t*)q, q_stride, out, 2, part_o, part_ml, (int32_t*)workspace, status);
+                     kv.k, kv.v, kv.ks, kv.vs, Hq, kv.Hkv, scale_log2e, (const uint16_t*)q, q_stride, out, 32, parts, status);
 }
 }  // namespace
 
 size_t kvq_attention_workspace(int Hq, int Hkv, int D, int q_max) {
-  size_t most = partial_floats(false, D);
-  if (is_wide(Hq / Hkv, q_max) && partial_floats(true, D) > most) most = partial_floats(true, D);
-  return kCounters * sizeof(int32_t) + most * sizeof(float);
+  const size_t few = workspace_bytes(false, D), many = is_wide(Hq / Hkv, q_max) ? workspace_bytes(true, D) : 0;
+  return few > many ? few : many;
 }
 
 void launch_kvq_attention(const KvqView& kv, const KvqSeqs& s, int Hq, const void* qrows, size_t q_stride, void* out, int32_t* status, void* workspace, hipStream_t st) {
