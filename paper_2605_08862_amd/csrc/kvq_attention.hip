@@ -43,8 +43,14 @@ __device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
 constexpr int kUnitCost = 24, kSnap = 2;
 template <bool WIDE> __device__ __forceinline__ int step_cost(int R) { return WIDE && R > 64 ? 14 : 8; }
 template <bool WIDE> constexpr int kBlock = WIDE ? 128 : 32;          // rows of a block
+// Query heads of a KV head.  x / g by a product with 2^32 / g rounded up: exact for x below 2^32 / g, i.e. any packed row.
+struct Group {
+  int g;
+  uint32_t recip;
+  __device__ __forceinline__ int div(int x) const { return g == 1 ? x : (int)__umulhi((uint32_t)x, recip); }
+};
 // Steps of the block qb of a sequence of n rows behind c tokens: of the tokens that its last row sees.
-template <int RP> __device__ __forceinline__ int block_steps(int c, int n, int G, int qb) { return (c + min(n - 1, ((qb + 1) * RP - 1) / G) + kStep) / kStep; }
+template <int RP> __device__ __forceinline__ int block_steps(int c, int n, Group G, int qb) { return (c + min(n - 1, G.div((qb + 1) * RP - 1)) + kStep) / kStep; }
 
 struct Shares {
   int total, W;                                         // length of everything, workgroups that have a share
@@ -64,26 +70,30 @@ struct Shares {
 // A share is no shorter than `least`, and longer than a step, so that every share between two others of a unit has a step of it.
 template <int THREADS, bool WIDE>
 __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
-                                              int n_max, int B, int n_slots, int max_pages, int G, int Hkv, int least, int* s_start, int* s_row, int* s_scan,
+                                              int n_max, int B, int n_slots, int max_pages, Group G, int Hkv, int least, int* s_start, int* s_row, int* s_scan,
                                               int32_t* __restrict__ status) {
   constexpr int NW = THREADS / 64, RP = kBlock<WIDE>;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (B + THREADS - 1) / THREADS, lo = min(tid * per, B), hi = min(lo + per, B);
+  // few sequences: up to 64 threads share the blocks of one, and the first of them has its place in the prefix sum; many: a thread has a run of them
+  int subs = 1;
+  while (subs < 64 && 2 * subs * B <= THREADS) subs *= 2;
+  const int per = subs > 1 ? 1 : (B + THREADS - 1) / THREADS, sub = tid & (subs - 1), at = tid / subs;
+  const int lo = min(at * per, B), hi = min(lo + per, B);
   int cost = 0, rows = 0, fault = 0;
   for (int b = lo; b < hi; ++b) {
-    s_start[b] = cost;
-    s_row[b] = rows;
+    if (sub == 0) { s_start[b] = cost; s_row[b] = rows; }
     const int n = seq_n[b] + n_add, slot = seq_slot[b], c = seq_pos[b];
     if (n < 0 || n > n_max) { fault |= BS_FAULT_DRAFT_LEN; continue; }
     if (n == 0) continue;
-    rows += n;
+    if (sub == 0) rows += n;
     if (slot < 0 || slot >= n_slots) { fault |= BS_FAULT_SLOT; continue; }
     if (c < 0 || (long long)c + n > (long long)max_pages * kPage) { fault |= BS_FAULT_KV_PAGES; continue; }
-    const int blocks = (n * G + RP - 1) / RP;
     int s = 0;
-    for (int qb = 0; qb < blocks; ++qb) s += kUnitCost + step_cost<WIDE>(n * G - qb * RP) * block_steps<RP>(c, n, G, qb);
+    for (int qb = sub; qb * RP < n * G.g; qb += subs) s += kUnitCost + step_cost<WIDE>(n * G.g - qb * RP) * block_steps<RP>(c, n, G, qb);
     cost += s * Hkv;
   }
+  for (int o = 1; o < subs; o <<= 1) cost += __shfl_xor(cost, o);
+  if (sub > 0) cost = 0;
   if (fault && blockIdx.x == 0 && status) atomicOr(status, fault);
   int is = cost, ir = rows;                             // exclusive prefix over the threads
 #pragma unroll
@@ -99,7 +109,8 @@ __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_sl
     if (w < wave) { bs += s_scan[w]; br += s_scan[NW + w]; }
     total += s_scan[w];
   }
-  for (int b = lo; b < hi; ++b) { s_start[b] += bs; s_row[b] += br; }
+  if (sub == 0)
+    for (int b = lo; b < hi; ++b) { s_start[b] += bs; s_row[b] += br; }
   if (tid == 0) s_start[B] = total;
   __syncthreads();
   Shares sh;
@@ -117,7 +128,7 @@ struct Unit {
   __device__ __forceinline__ int end() const { return first + kUnitCost + step * steps; }
   // step at which a cut at p is made
   __device__ __forceinline__ int cut(int p) const {
-    const int j = (p - first - kUnitCost + step - 1) / step;
+    const int x = max(p - first - kUnitCost, 0) + step - 1, j = step == 8 ? x >> 3 : (int)__umulhi((uint32_t)x, 306783379u);   // / step, 8 or 14
     return p >= end() ? steps : p <= first + kUnitCost + kSnap * step ? 0 : steps - j <= kSnap ? steps : j;
   }
   // the first and the last workgroup that have steps of the unit
@@ -125,33 +136,36 @@ struct Unit {
   __device__ __forceinline__ int last_share(const Shares& sh) const { return sh.of(first + kUnitCost + max(step * (steps - kSnap - 1), kSnap * step)); }
 };
 template <bool WIDE>
-__device__ __forceinline__ void fill_unit(Unit& u, int G) {
+__device__ __forceinline__ void fill_unit(Unit& u, Group G) {
   constexpr int RP = kBlock<WIDE>;
   u.steps = block_steps<RP>(u.c, u.n, G, u.qb);
-  u.step = step_cost<WIDE>(u.n * G - u.qb * RP);
+  u.step = step_cost<WIDE>(u.n * G.g - u.qb * RP);
 }
 template <bool WIDE>
-__device__ __forceinline__ void enter_sequence(Unit& u, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add, int G) {
+__device__ __forceinline__ void enter_sequence(Unit& u, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add, Group G) {
   u.b = __builtin_amdgcn_readfirstlane(u.b);
   u.n = seq_n[u.b] + n_add;
   u.c = seq_pos[u.b];
   u.row0 = __builtin_amdgcn_readfirstlane(s_row[u.b]);
   u.first = __builtin_amdgcn_readfirstlane(s_start[u.b]);
-  u.blocks = (u.n * G + kBlock<WIDE> - 1) / kBlock<WIDE>;
+  u.blocks = (u.n * G.g + kBlock<WIDE> - 1) / kBlock<WIDE>;
   u.h = u.qb = 0;
   fill_unit<WIDE>(u, G);
 }
 // The unit that p (below the total) lies in.
 template <bool WIDE>
 __device__ __forceinline__ Unit unit_at(int p, int B, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
-                                        int G, int Hkv) {
+                                        Group G, int Hkv) {
   Unit u;
   int lo = 0, hi = B;                                   // largest b with s_start[b] <= p (sequences without units are passed over)
   while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_start[mid] <= p) lo = mid; else hi = mid; }
   u.b = lo;
   enter_sequence<WIDE>(u, s_start, s_row, seq_pos, seq_n, n_add, G);
-  const int head = __builtin_amdgcn_readfirstlane((s_start[u.b + 1] - u.first) / Hkv);
-  u.h = (p - u.first) / head;
+  const int all = __builtin_amdgcn_readfirstlane(s_start[u.b + 1]) - u.first, head = u.blocks == 1 ? u.end() - u.first : all / Hkv;
+  int h = min(Hkv - 1, (int)((float)(p - u.first) / (float)head));
+  while (h > 0 && h * head > p - u.first) --h;
+  while (h + 1 < Hkv && (h + 1) * head <= p - u.first) ++h;
+  u.h = __builtin_amdgcn_readfirstlane(h);
   u.first += u.h * head;
   while (u.end() <= p) { u.first = u.end(); ++u.qb; fill_unit<WIDE>(u, G); }
   return u;
@@ -159,7 +173,7 @@ __device__ __forceinline__ Unit unit_at(int p, int B, const int* s_start, const 
 // The unit behind; false behind the last one.
 template <bool WIDE>
 __device__ __forceinline__ bool next_unit(Unit& u, int B, int Hkv, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n,
-                                          int n_add, int G) {
+                                          int n_add, Group G) {
   u.first = u.end();
   if (++u.qb < u.blocks) { fill_unit<WIDE>(u, G); return true; }
   u.qb = 0;
@@ -175,15 +189,15 @@ struct Part {
   bool whole;
 };
 template <bool WIDE>
-__device__ __forceinline__ Part part_of(const Unit& u, const Shares& sh, int s_lo, int s_hi, int G) {
+__device__ __forceinline__ Part part_of(const Unit& u, const Shares& sh, int s_lo, int s_hi, Group G) {
   constexpr int RP = kBlock<WIDE>;
   Part t;
   t.b = u.b; t.h = u.h; t.row0 = u.row0; t.c = u.c;
   t.qr0 = u.qb * RP;
-  t.R = min(u.n * G - t.qr0, RP);
+  t.R = min(u.n * G.g - t.qr0, RP);
   t.s_lo = s_lo; t.s_hi = s_hi;
-  t.n_tiles = (u.c + min(u.n - 1, (t.qr0 + RP - 1) / G)) / kTile + 1;
-  t.c_all = u.c + t.qr0 / G;
+  t.n_tiles = (u.c + min(u.n - 1, G.div(t.qr0 + RP - 1))) / kTile + 1;
+  t.c_all = u.c + G.div(t.qr0);
   t.whole = s_lo == 0 && s_hi == u.steps;
   t.w_first = t.w_last = blockIdx.x;
   if (!t.whole) {
@@ -195,7 +209,7 @@ __device__ __forceinline__ Part part_of(const Unit& u, const Shares& sh, int s_l
 // Calls f(part) for every part of this workgroup's share.
 template <bool WIDE, typename F>
 __device__ __forceinline__ void for_parts(const Shares& sh, int B, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n,
-                                          int n_add, int G, int Hkv, const F& f) {
+                                          int n_add, Group G, int Hkv, const F& f) {
   const int w = blockIdx.x;
   if (w >= sh.W || sh.total == 0) return;
   const int p0 = __builtin_amdgcn_readfirstlane(sh.bound(w)), p1 = __builtin_amdgcn_readfirstlane(sh.bound(w + 1));
@@ -222,6 +236,13 @@ __device__ __forceinline__ void store4(const KvqOut& out, int Hq, int row, int c
   }
 }
 
+// Four columns of row r of a block.
+template <int D, bool STEP>
+__device__ __forceinline__ void store_row(const KvqOut& out, int Hq, const Part& un, Group G, int r, int col, f32x4 v, float inv, int32_t* status) {
+  const int qr = un.qr0 + r, i = G.div(qr);
+  store4<D, STEP>(out, Hq, un.row0 + i, (un.h * G.g + qr - i * G.g) * D + col, v, inv, status);
+}
+
 // ---- merge of a unit's parts -------------------------------------------------------------------------------------------------------
 // Partial rows: part_o [2 W][RP][D], and (maximum, sum) part_ml [kLevels][2 W][RP][2].  Parts are merged in groups of F neighbours by the last of a group to
 // arrive, into the place of the group's first part, the merged parts again, and so on: a unit of 64 parts of 119 rows is 4 MB, which one workgroup alone read in
@@ -234,7 +255,7 @@ template <int RP> constexpr uint32_t kMlLevel = (uint32_t)2 * kMaxShares * RP;  
 // Merges `count` parts, `stride` apart from part i0 of the unit on, on level `level`.  An item is four columns of a row; the loads of NI items and GC parts are in
 // flight together.
 template <int THREADS, int RP, int D, bool STEP, int NI, int GC>
-__device__ __forceinline__ void merge_group(const Part& un, const Parts& p, int level, int i0, int stride, int count, bool last, const KvqOut& out, int Hq, int G,
+__device__ __forceinline__ void merge_group(const Part& un, const Parts& p, int level, int i0, int stride, int count, bool last, const KvqOut& out, int Hq, Group G,
                                             int32_t* status) {
   constexpr int CH = D / 4;
   const wt_buf bo = wt_buffer(p.o), bm = wt_buffer(p.ml);
@@ -288,15 +309,14 @@ __device__ __forceinline__ void merge_group(const Part& un, const Parts& p, int 
         wt_store4(bo, ((to + r) * D + ch * 4) * 4, acc[k]);
         if (ch == 0) wt_store2(bm, ((level + 1) * kMlLevel<RP> + to + r) * 8, m[k], l[k]);
       } else if (m[k] != INFINITY) {                    // (infinite: a bad page, the row stays as it is)
-        const int qr = un.qr0 + r;
-        store4<D, STEP>(out, Hq, un.row0 + qr / G, (un.h * G + qr % G) * D + ch * 4, acc[k], 1.0f / l[k], status);
+        store_row<D, STEP>(out, Hq, un, G, r, ch * 4, acc[k], 1.0f / l[k], status);
       }
     }
   }
 }
 // Called by all threads of a workgroup that has stored its part of a cut unit on level 0.
 template <int THREADS, int RP, int D, bool STEP>
-__device__ __forceinline__ void merge_unit(const Part& un, const Parts& p, const KvqOut& out, int Hq, int G, int32_t* status, int* s_flag) {
+__device__ __forceinline__ void merge_unit(const Part& un, const Parts& p, const KvqOut& out, int Hq, Group G, int32_t* status, int* s_flag) {
   const bool few = un.R * (D / 4) <= THREADS;           // few rows, as of one long sequence
   const int F = few ? 8 : 4, n = un.w_last - un.w_first + 1;
   int i = (int)blockIdx.x - un.w_first;
@@ -375,7 +395,7 @@ template <bool STEP> __device__ __forceinline__ u32x4 query8(u32x4 v, bool& rang
 #define BS_KVQ_PARAMS                                                                                                                                     \
   const int32_t *__restrict__ seq_slot, const int32_t *__restrict__ seq_pos, const int32_t *__restrict__ seq_n, int n_add, int n_max, int B,                \
       const int32_t *__restrict__ block_table, int n_slots, int max_pages, int n_pages, const uint8_t *__restrict__ k_pages, const uint8_t *__restrict__ v_pages, \
-      const float *__restrict__ k_scale, const float *__restrict__ v_scale, int Hq, int Hkv, float scale_log2e, const uint16_t *__restrict__ q, size_t q_stride, \
+      const float *__restrict__ k_scale, const float *__restrict__ v_scale, int Hq, int Hkv, int g_n, uint32_t g_recip, float scale_log2e, const uint16_t *__restrict__ q, size_t q_stride, \
       KvqOut out, int least, Parts parts, int32_t *__restrict__ status
 
 // Blocks of up to 32 NQ rows, four waves.  STEP: inside bs_verify_step (float16 queries, output in chunk order).
@@ -392,7 +412,8 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) kvq_attention_kernel(BS_
   float* const s_l = s_m + 4 * RP;
   int* const s_start = (int*)(s_l + 4 * RP);            // [B + 1]
   int* const s_row = s_start + B + 1;                   // [B + 1]
-  const int tid = threadIdx.x, G = Hq / Hkv, w_id = blockIdx.x;
+  const int tid = threadIdx.x, w_id = blockIdx.x;
+  const Group G{g_n, g_recip};
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, ln = lane & 31, lg = lane >> 5;
   const Shares sh = find_shares<256, false>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, least, s_start, s_row, s_scan, status);
   for_parts<false>(sh, B, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv, [&](const Part& un) {
@@ -419,8 +440,8 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) kvq_attention_kernel(BS_
 #pragma unroll
     for (int j = 0; j < QF; ++j) {
       const int f = wave + 4 * j, qt = f / KS, s = f % KS;
-      const int qr = un.qr0 + min(qt * 32 + ln, un.R - 1);    // rows behind the last one are masked
-      qv[j] = *(const u32x4*)(q + (size_t)(un.row0 + qr / G) * q_stride + (size_t)(un.h * G + qr % G) * D + lg * (D / 2) + s * 8);
+      const int qr = un.qr0 + min(qt * 32 + ln, un.R - 1), i = G.div(qr);    // rows behind the last one are masked
+      qv[j] = *(const u32x4*)(q + (size_t)(un.row0 + i) * q_stride + (size_t)(un.h * G.g + qr - i * G.g) * D + lg * (D / 2) + s * 8);
     }
     u32x4 k0[DT], v0[DT], k1[DT], v1[DT];
     At a0 = place(n_my > 0 ? t0 : un.n_tiles - 1), a1 = place(n_my > 1 ? t0 + 4 : n_my > 0 ? t0 : un.n_tiles - 1);
@@ -442,7 +463,7 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) kvq_attention_kernel(BS_
     for (int qt = 0; qt < NQ; ++qt) {
       m_run[qt] = -INFINITY;
       l_run[qt] = 0.f;
-      lim[qt] = qt * 32 + ln < un.R ? un.c + (un.qr0 + qt * 32 + ln) / G : -1;
+      lim[qt] = qt * 32 + ln < un.R ? un.c + G.div(un.qr0 + qt * 32 + ln) : -1;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -535,8 +556,7 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) kvq_attention_kernel(BS_
           wt_store4(bo, ((part + rr) * D + ch * 4) * 4, acc);
           if (ch == 0) wt_store2(bm, (part + rr) * 8, mt, lt);
         } else if (mt != INFINITY) {
-          const int qr = un.qr0 + rr;
-          store4<D, STEP>(out, Hq, un.row0 + qr / G, (un.h * G + qr % G) * D + ch * 4, acc, 1.0f / lt, status);
+          store_row<D, STEP>(out, Hq, un, G, rr, ch * 4, acc, 1.0f / lt, status);
         }
       }
     }
@@ -573,7 +593,8 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
   float* const s_l = s_m + 8 * 32;
   int* const s_start = (int*)(s_l + 8 * 32);            // [B + 1]
   int* const s_row = s_start + B + 1;                   // [B + 1]
-  const int tid = threadIdx.x, G = Hq / Hkv, w_id = blockIdx.x;
+  const int tid = threadIdx.x, w_id = blockIdx.x;
+  const Group G{g_n, g_recip};
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, ln = lane & 31, lg = lane >> 5;
   const Shares sh = find_shares<512, true>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, least, s_start, s_row, s_scan, status);
 
@@ -604,11 +625,11 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
       }
     };
     const int qr = qt * 32 + ln;
-    const int lim = qr < un.R ? un.c + (un.qr0 + qr) / G : -1;
+    const int lim = qr < un.R ? un.c + G.div(un.qr0 + qr) : -1;
     u32x4 qf[KS];
     {
-      const int qc = un.qr0 + min(qr, un.R - 1);
-      const uint16_t* src = q + (size_t)(un.row0 + qc / G) * q_stride + (size_t)(un.h * G + qc % G) * D + lg * (D / 2);
+      const int qc = un.qr0 + min(qr, un.R - 1), i = G.div(qc);
+      const uint16_t* src = q + (size_t)(un.row0 + i) * q_stride + (size_t)(un.h * G.g + qc - i * G.g) * D + lg * (D / 2);
 #pragma unroll
       for (int s = 0; s < KS; ++s) qf[s] = *(const u32x4*)(src + s * 8);
     }
@@ -707,8 +728,7 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
           wt_store4(bo, ((part + r) * D + col) * 4, acc);
           if (half == 0 && ch == 0) wt_store2(bm, (part + r) * 8, bad_unit ? INFINITY : mt, lt);
         } else if (!bad_unit) {
-          const int rr = un.qr0 + r;
-          store4<D, STEP>(out, Hq, un.row0 + rr / G, (un.h * G + rr % G) * D + col, acc, 1.0f / lt, status);
+          store_row<D, STEP>(out, Hq, un, G, r, col, acc, 1.0f / lt, status);
         }
       }
     }
@@ -728,10 +748,11 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
 }
 
 // Blocks of 32 rows on four waves, two workgroups on a CU, or of up to 128 rows on eight waves.  The second reads K/V once for four times the rows, but has
-// more to do before and behind its steps, so it needs many units: 7B heads, 17 rows, 32 units of 20000 tokens 68 us on the first and 75 on the second, 64 of
+// more to do before and behind its steps, so it needs many
+// units (of 128 rows): 7B heads, 17 rows, 32 units of 20000 tokens 68 us on the first and 75 on the second, 64 of
 // 8000 93 and 64; 1.5B heads, 9 rows, 32 units of 8000 27 and 32; 7B heads, 9 rows, 128 of 8192 94 and 70.
 bool is_wide(int G, int q_max) { return (long long)q_max * G > 32; }
-bool runs_wide(const KvqSeqs& s, int G, int Hkv) { return is_wide(G, s.n_max) && s.B * Hkv > 32; }
+bool runs_wide(const KvqSeqs& s, int G, int Hkv) { return is_wide(G, s.n_max) && s.B * Hkv * (((long long)s.n_max * G + 127) / 128) > 32; }
 int workgroups(bool wide) { return (wide ? 1 : 2) * kCUs; }
 size_t workspace_bytes(bool wide, int D) {
   const size_t rows = (size_t)2 * (wide ? 128 : 32);
@@ -741,7 +762,11 @@ size_t workspace_bytes(bool wide, int D) {
 template <int D, bool STEP>
 void launch(const KvqView& kv, const KvqSeqs& s, int Hq, const void* q, size_t q_stride, KvqOut out, int32_t* status, void* workspace, hipStream_t st) {
   const bool wide = runs_wide(s, Hq / kv.Hkv, kv.Hkv);
-  const int grid = workgroups(wide), RP = wide ? 128 : 32;
+  const int RP = wide ? 128 : 32, G = Hq / kv.Hkv, least = 32;
+  // no more workgroups than shares, of sequences as long as the block table is wide
+  const long long blocks = ((long long)s.n_max * G + RP - 1) / RP, most = (long long)s.B * kv.Hkv * blocks * (kUnitCost + 14 * (kv.max_pages / 2 + 1)) / least + 1;
+  const int grid = (int)(most < workgroups(wide) ? most : workgroups(wide));
+  const uint32_t g_recip = G == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + G - 1) / G);
   int32_t* counters = (int32_t*)workspace;
   float* ml = (float*)(counters + kLevels * kMaxShares);
   const Parts parts{ml + (size_t)kLevels * 2 * kMaxShares * RP * 2, ml, counters};
@@ -753,7 +778,7 @@ void launch(const KvqView& kv, const KvqSeqs& s, int Hq, const void* q, size_t q
   (void)set;
   const float scale_log2e = 1.4426950408889634f / sqrtf((float)D);
   hipLaunchKernelGGL(kern, dim3(grid), dim3(wide ? 512 : 256), lds, st, s.slot, s.pos, s.n, s.n_add, s.n_max, s.B, kv.block_table, kv.n_slots, kv.max_pages, kv.n_pages,
-                     kv.k, kv.v, kv.ks, kv.vs, Hq, kv.Hkv, scale_log2e, (const uint16_t*)q, q_stride, out, 32, parts, status);
+                     kv.k, kv.v, kv.ks, kv.vs, Hq, kv.Hkv, G, g_recip, scale_log2e, (const uint16_t*)q, q_stride, out, least, parts, status);
 }
 }  // namespace
 
