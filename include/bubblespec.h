@@ -330,8 +330,8 @@ bs_status bs_kvq_attention(const bs_kvq_desc* kv, int B, const int32_t* seq_slot
  * n_tokens is out of range (BS_FAULT_DRAFT_LEN; a draft_len outside [0, k_max] counts no rows).  status: as above.
  * workspace (dev, 256-byte aligned, at least bs_token_logprobs_workspace_bytes of the same vocab and n_top and of B and k_max no smaller) is zero-filled
  * once before its first use; calls that share one must not overlap in time.
- * Errors: BS_EINVAL (null, temperature or its reciprocal not in (0, inf), bad dtype, logits not aligned to their elements), BS_ESHAPE (vocab < 2 or > 2^24, n_top outside
- * [0, 32] or above vocab, B or k_max + 1 outside [1, 4096], more than 2^20 rows), BS_ECAPACITY (workspace too small), BS_EHIP. */
+ * Errors: BS_EINVAL (null, temperature or its reciprocal not in (0, inf), bad dtype, logits not aligned to their elements), BS_ESHAPE (vocab < 2 or > 2^20, n_top outside
+ * [0, 32] or above vocab, B or k_max + 1 outside [1, 4096], more than 2^16 rows), BS_ECAPACITY (workspace too small), BS_EHIP. */
 size_t bs_token_logprobs_workspace_bytes(int B, int k_max, int vocab, int n_top);   /* 0 on invalid arguments */
 bs_status bs_token_logprobs(int B, int vocab, const void* logits, int logits_dtype, const int32_t* draft_len /*[B] or NULL*/,
                             int k_max, const int32_t* tokens /*[B,k_max+1]*/, const int32_t* n_tokens /*[B] or NULL*/,

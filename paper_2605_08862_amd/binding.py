@@ -263,24 +263,35 @@ def bs_kv_read(ctx, layer, slot, pos0, n, k_rows, v_rows):
     _check(ctx, lib().bs_kv_read(ctx, layer, slot, pos0, n, _ptr(k_rows), _ptr(v_rows), _stream()))
 
 
-def _on_current_device(*tensors):
-    """The calls without a context launch on the current device's stream: a tensor of another device is refused."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
-            raise BsError(BS_EINVAL, "tensor on %s, current device cuda:%d" % (t.device, dev))
+def _here(t, dev):
+    """Address of a dense tensor on device `dev` (None: NULL).  The calls without a context launch on the current device's stream: a
+    tensor of another device is refused."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise BsError(BS_EINVAL, "tensor on %s, current device cuda:%d" % (t.device, dev))
+    if not t.is_contiguous():
+        raise BsError(BS_EINVAL, "a dense tensor is expected")
+    return t.data_ptr()
 
 
-def _rows(t, width):
+def _rows(t, width, dev):
     """(address, elements from one row to the next) of packed rows [n, ..., ...] whose inner dimensions are dense."""
+    if t.get_device() != dev:
+        raise BsError(BS_EINVAL, "tensor on %s, current device cuda:%d" % (t.device, dev))
+    if t.dtype != torch.bfloat16:
+        raise BsError(BS_EINVAL, "rows are bfloat16")
+    n = t.shape[0]
+    if n * width != t.numel():
+        raise BsError(BS_ESHAPE, "rows of %s elements, %d expected" % (tuple(t.shape[1:]), width))
+    if t.is_contiguous():
+        return t.data_ptr(), width
     inner = 1
     for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
         if size != 1 and stride != inner:
             raise BsError(BS_EINVAL, "the inner dimensions of the rows must be dense")
         inner *= size
-    if inner != width:
-        raise BsError(BS_ESHAPE, "rows of %d elements, %d expected" % (inner, width))
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else width)
+    return t.data_ptr(), t.stride(0)
 
 
 def make_kvq_desc(kv):
@@ -291,14 +302,13 @@ def make_kvq_desc(kv):
 
 
 def _kvq_copy(name, desc, B, seq_slot, pos0, n_rows, n_max, k_rows, v_rows, status):
-    _on_current_device(seq_slot, pos0, n_rows, k_rows, v_rows, status)
+    dev = torch.cuda.current_device()
     width = desc.n_kv_heads * desc.head_dim
-    if k_rows.dtype != torch.bfloat16 or v_rows.dtype != torch.bfloat16:
-        raise BsError(BS_EINVAL, name + ": rows are bfloat16")
-    (k, ks), (v, vs) = _rows(k_rows, width), _rows(v_rows, width)
-    if ks != vs:
-        raise BsError(BS_EINVAL, name + ": K and V rows must have the same stride")
-    st = getattr(lib(), name)(C.byref(desc), B, _ptr(seq_slot), _ptr(pos0), _ptr(n_rows), n_max, k, v, ks, _ptr(status), _stream())
+    k, stride = _rows(k_rows, width, dev)
+    v, v_stride = _rows(v_rows, width, dev)
+    if stride != v_stride or k_rows.shape[0] != v_rows.shape[0]:
+        raise BsError(BS_EINVAL, name + ": K and V rows must have the same number and stride")
+    st = getattr(lib(), name)(C.byref(desc), B, _here(seq_slot, dev), _here(pos0, dev), _here(n_rows, dev), n_max, k, v, stride, _here(status, dev), _stream())
     if st != BS_OK:
         raise BsError(st, name)
 
@@ -316,12 +326,12 @@ def bs_kvq_workspace_bytes(n_q_heads, n_kv_heads, head_dim, q_max):
 
 
 def bs_kvq_attention(desc, B, seq_slot, ctx_len, q_len, q_max, n_q_heads, q, out, workspace, status=None):
-    _on_current_device(seq_slot, ctx_len, q_len, q, out, workspace, status)
-    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
-        raise BsError(BS_EINVAL, "bs_kvq_attention: q and out are bfloat16")
-    address, stride = _rows(q, n_q_heads * desc.head_dim)
-    st = lib().bs_kvq_attention(C.byref(desc), B, _ptr(seq_slot), _ptr(ctx_len), _ptr(q_len), q_max, n_q_heads, address, stride, _ptr(out), _ptr(status),
-                                _ptr(workspace), workspace.numel() * workspace.element_size(), _stream())
+    dev = torch.cuda.current_device()
+    address, stride = _rows(q, n_q_heads * desc.head_dim, dev)
+    if out.dtype != torch.bfloat16 or out.numel() < q.numel():
+        raise BsError(BS_EINVAL, "bs_kvq_attention: out is bfloat16, with a row for every row of q")
+    st = lib().bs_kvq_attention(C.byref(desc), B, _here(seq_slot, dev), _here(ctx_len, dev), _here(q_len, dev), q_max, n_q_heads, address, stride, _here(out, dev),
+                                _here(status, dev), _here(workspace, dev), workspace.numel() * workspace.element_size(), _stream())
     if st != BS_OK:
         raise BsError(st, "bs_kvq_attention")
 
@@ -332,11 +342,11 @@ def bs_token_logprobs_workspace_bytes(B, k_max, vocab, n_top):
 
 def bs_token_logprobs(B, vocab, logits, draft_len, k_max, tokens, n_tokens, temperature, n_top, logprob, entropy, top_tokens, top_logprobs,
                       workspace, status=None):
-    _on_current_device(logits, draft_len, tokens, n_tokens, logprob, entropy, top_tokens, top_logprobs, workspace, status)
-    dtype = {torch.float32: BS_F32, torch.bfloat16: BS_BF16}.get(logits.dtype, -1)
-    st = lib().bs_token_logprobs(B, vocab, _ptr(logits), dtype, _ptr(draft_len), k_max, _ptr(tokens), _ptr(n_tokens), temperature, n_top, _ptr(logprob),
-                                 _ptr(entropy), _ptr(top_tokens), _ptr(top_logprobs), _ptr(status), _ptr(workspace),
-                                 workspace.numel() * workspace.element_size(), _stream())
+    dev = torch.cuda.current_device()
+    dtype = BS_F32 if logits.dtype == torch.float32 else BS_BF16 if logits.dtype == torch.bfloat16 else -1
+    st = lib().bs_token_logprobs(B, vocab, _here(logits, dev), dtype, _here(draft_len, dev), k_max, _here(tokens, dev), _here(n_tokens, dev), temperature, n_top,
+                                 _here(logprob, dev), _here(entropy, dev), _here(top_tokens, dev), _here(top_logprobs, dev), _here(status, dev),
+                                 _here(workspace, dev), workspace.numel() * workspace.element_size(), _stream())
     if st != BS_OK:
         raise BsError(st, "bs_token_logprobs")
 

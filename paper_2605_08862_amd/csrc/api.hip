@@ -791,7 +791,7 @@ bs_status bs_kvq_attention(const bs_kvq_desc* kv, int B, const int32_t* seq_slot
 }
 
 size_t bs_token_logprobs_workspace_bytes(int B, int k_max, int vocab, int n_top) {
-  if (B < 1 || B > 4096 || k_max < 0 || k_max > 4095 || B * (k_max + 1) > (1 << 20) || vocab < 2 || vocab > (1 << 24) || n_top < 0 || n_top > kLogprobMaxTop || n_top > vocab)
+  if (B < 1 || B > 4096 || k_max < 0 || k_max > 4095 || B * (k_max + 1) > kLogprobMaxRows || vocab < 2 || vocab > kLogprobMaxVocab || n_top < 0 || n_top > kLogprobMaxTop || n_top > vocab)
     return 0;
   return logprob_workspace(B, k_max, vocab, n_top);
 }

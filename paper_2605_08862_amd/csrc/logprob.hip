@@ -2,87 +2,285 @@
 //
 // With m = max z and y = (z - m) / T:  log p(t) = y_t - log sum e^y,  H = log sum e^y - sum e^y y / sum e^y.  A masked token (-inf) has e^y = 0 and adds
 // nothing to either sum.  A row in which everything is masked has no law: log p = -inf, H = 0, no alternatives.
+//
+// One pass over the logits, bound by memory.  A row is cut into segments, a workgroup each, which keeps its segment in registers: every wave sums against its own
+// maximum, and the best alternatives come from a bound.  The largest of 64 groups of threads are known from the maxima; the n-th largest of these is no larger
+// than the n-th largest logit, and hardly any other logit reaches it, so that one comparison per logit leaves a short list (a few more than n), which is ranked by
+// counting.  The last segment of a row to arrive (publish_arrival, common.h) merges maxima, sums and lists the same way.
 #include "logprob.h"
 
 namespace {
-template <typename T>
-__global__ void __launch_bounds__(256) logprob_kernel(LogprobArgs a) {
-  __shared__ float s_f[12];
-  __shared__ unsigned long long s_u[4];
-  __shared__ int s_i[4];
-  const int b = blockIdx.x / (a.k_max + 1), i = blockIdx.x % (a.k_max + 1), tid = threadIdx.x, V = a.vocab;
+
+constexpr int kThreads = 256, kVecs = 16, kList = 512;  // vectors of sixteen bytes of a thread; places of the list of candidates
+constexpr int kMaxSegs = kLogprobMaxVocab / (kThreads * 64);
+constexpr int kMergeEach = kMaxSegs * kLogprobMaxTop / kThreads;     // list entries of a thread in the merge
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t u16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+template <typename T> constexpr int kPer = 16 / sizeof(T);                    // elements of a vector
+
+struct Top { float z; int j; };
+__device__ __forceinline__ bool better(float za, int ja, float zb, int jb) { return za > zb || (za == zb && ja < jb); }
+
+struct SelectShared {
+  float group[4][64];
+  Top list[kList];
+  int n;
+  Top best[4];
+};
+
+// The n best of the elements that the threads hold in z (E each, their indexes by `index`), -inf and NaN are none.  out(rank, z, j) is called once for every
+// rank that is taken; returns how many are.  zmax: largest z of the thread.
+template <int E, typename Index, typename Out>
+__device__ __forceinline__ int select_top(const float (&z)[E], float zmax, int n, const Index& index, const Out& out, SelectShared& s) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  s.group[wave][lane] = zmax;
+  if (tid == 0) s.n = 0;
+  __syncthreads();
+  // bound: the n-th largest of the 64 groups (a lane of all four waves); equal ones in the order of the lanes
+  const float g = fmaxf(fmaxf(s.group[0][lane], s.group[1][lane]), fmaxf(s.group[2][lane], s.group[3][lane]));
   int before = 0;
-  for (int x = tid; x < b; x += 256) { const int k = a.draft_len ? a.draft_len[x] : a.k_max; before += k >= 0 && k <= a.k_max ? k + 1 : 0; }
+#pragma unroll
+  for (int o = 0; o < 64; ++o) {
+    const float x = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), o));
+    before += x > g || (x == g && o < lane) ? 1 : 0;
+  }
+  const unsigned long long at = __ballot(before == n - 1);
+  const float bound = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), __ffsll((long long)at) - 1));
+  if (__any(zmax >= bound && zmax > -INFINITY)) {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (z[e] >= bound && z[e] > -INFINITY) {
+        const int k = atomicAdd(&s.n, 1);
+        if (k < kList) s.list[k] = Top{z[e], index(e)};
+      }
+  }
+  __syncthreads();
+  const int found = s.n;
+  if (found <= kList) {
+    for (int k = tid; k < found; k += kThreads) {
+      const Top t = s.list[k];
+      int rank = 0;
+      for (int o = 0; o < found; ++o) { const Top x = s.list[o]; rank += better(x.z, x.j, t.z, t.j) ? 1 : 0; }
+      if (rank < n) out(rank, t.z, t.j);
+    }
+    return min(found, n);
+  }
+  // more than the list holds reach the bound (a segment of equal logits, say): one after the other
+  Top last{INFINITY, -1};
+  for (int r = 0; r < n; ++r) {
+    Top best{-INFINITY, 0x7fffffff};
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int j = index(e);
+      if (better(last.z, last.j, z[e], j) && better(z[e], j, best.z, best.j)) best = Top{z[e], j};
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const float x = __shfl_xor(best.z, o);
+      const int j = __shfl_xor(best.j, o);
+      if (better(x, j, best.z, best.j)) best = Top{x, j};
+    }
+    __syncthreads();
+    if (lane == 0) s.best[wave] = best;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) if (better(s.best[w].z, s.best[w].j, best.z, best.j)) best = s.best[w];
+    last = best;
+    if (tid == 0) out(r, best.z, best.j);
+  }
+  return n;
+}
+
+// Maximum and sums of a part of a row, in units of log2: t = (z - m) c with c = log2(e) / T;  s = sum 2^t, q = sum 2^t t.
+struct Stats { float m, s, q; };
+__device__ __forceinline__ Stats merge_stats(Stats a, Stats b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  if (m == -INFINITY) return Stats{m, a.s + b.s, a.q + b.q};                  // both empty (or NaN alone, which the sums carry)
+  // a shift of the maximum by d moves every t by d c
+  const float da = a.m == -INFINITY ? 0.f : (a.m - m) * c, db = b.m == -INFINITY ? 0.f : (b.m - m) * c;
+  const float fa = a.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(da), fb = b.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(db);
+  const float qa = fmaxf(da, -1e4f), qb = fmaxf(db, -1e4f);                  // 0 * -inf is 0 here
+  return Stats{m, a.s * fa + b.s * fb, fa * (a.q + a.s * qa) + fb * (b.q + b.s * qb)};
+}
+
+// `entry`: the row's place in the outputs; false: it has no row, and its outputs are written.
+__device__ __forceinline__ bool find_row(const LogprobArgs& a, int entry, bool write, int* s_i, size_t& row, int& tok) {
+  const int width = a.k_max + 1, b = entry / width, i = entry - b * width, tid = threadIdx.x;
+  const int k = a.draft_len ? a.draft_len[b] : a.k_max, n = a.n_tokens ? a.n_tokens[b] : k + 1;
+  const bool bad = k < 0 || k > a.k_max || n < 0 || n > k + 1;
+  tok = !bad && i < n ? a.tokens[entry] : 0;
+  const bool wrong = tok < 0 || tok >= a.vocab;
+  if (bad || i >= n || wrong) {
+    if (!write) return false;
+    if (tid == 0) {
+      if (bad && i == 0 && a.status) atomicOr(a.status, BS_FAULT_DRAFT_LEN);
+      if (wrong && a.status) atomicOr(a.status, BS_FAULT_TOKEN_ID);
+      a.logprob[entry] = 0.f;
+      if (a.entropy) a.entropy[entry] = 0.f;
+    }
+    for (int j = tid; j < a.n_top; j += kThreads) { a.top_tokens[(size_t)entry * a.n_top + j] = -1; a.top_logprobs[(size_t)entry * a.n_top + j] = 0.f; }
+    return false;
+  }
+  if (!a.draft_len) { row = entry; return true; }
+  int before = 0;
+  for (int x = tid; x < b; x += kThreads) { const int d = a.draft_len[x]; before += d >= 0 && d <= a.k_max ? d + 1 : 0; }
+#pragma unroll
   for (int o = 1; o < 64; o <<= 1) before += __shfl_xor(before, o);
   if ((tid & 63) == 0) s_i[tid >> 6] = before;
   __syncthreads();
-  before = s_i[0] + s_i[1] + s_i[2] + s_i[3];
-  const int k = a.draft_len ? a.draft_len[b] : a.k_max, n = a.n_tokens ? a.n_tokens[b] : k + 1;
-  const size_t at = blockIdx.x;
-  const bool bad = k < 0 || k > a.k_max || n < 0 || n > k + 1;
-  if (bad && i == 0 && tid == 0 && a.status) atomicOr(a.status, BS_FAULT_DRAFT_LEN);
-  const int tok = !bad && i < n ? a.tokens[at] : -1;
-  const bool wrong = !bad && i < n && (tok < 0 || tok >= V);
-  if (wrong && tid == 0 && a.status) atomicOr(a.status, BS_FAULT_TOKEN_ID);
-  if (bad || i >= n || wrong) {
-    if (tid == 0) { a.logprob[at] = 0.f; if (a.entropy) a.entropy[at] = 0.f; }
-    for (int j = tid; j < a.n_top; j += 256) { a.top_tokens[at * a.n_top + j] = -1; a.top_logprobs[at * a.n_top + j] = 0.f; }
-    return;
+  row = (size_t)(s_i[0] + s_i[1] + s_i[2] + s_i[3]) + i;
+  return true;
+}
+
+// seg: elements of a segment, a multiple of 8; segs of them cover a row.  Partials: [entry][segs] statistics, [entry][segs][n_top] alternatives.
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kThreads) logprob_kernel(LogprobArgs a, int seg, int segs, wt_f32x4* __restrict__ part, Top* __restrict__ part_top,
+                                                           int32_t* __restrict__ counters) {
+  __shared__ SelectShared s_sel;
+  __shared__ Stats s_stats[4];
+  __shared__ Top s_top[kLogprobMaxTop];
+  __shared__ int s_i[4], s_flag;
+  constexpr int P = kPer<T>, E = kVecs * (P > 4 ? 4 : P);                     // elements of a thread: 64 whatever the type
+  constexpr int NV = E / P;                                                  // vectors
+  const int entry = blockIdx.x / segs, sg = blockIdx.x - entry * segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.vocab;
+  size_t row;
+  int tok;
+  if (!find_row(a, entry, sg == 0, s_i, row, tok)) return;
+  const T* z0 = (const T*)a.logits + row * V;
+  const int j0 = sg * seg, j1 = min(j0 + seg, V);
+  const float z_tok = to_f32<T>(z0[tok]);
+
+  // ---- the segment: element e of a thread is j0 + (e / P * kThreads + tid) * P + e % P
+  float z[E];
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int j = j0 + (u * kThreads + tid) * P;
+    if (j0 + u * kThreads * P >= j1) {                  // the same for all threads
+#pragma unroll
+      for (int e = 0; e < P; ++e) z[u * P + e] = -INFINITY;
+    } else if (j + P <= j1) {
+      if constexpr (P == 4) {
+        const f32x4_any v = *(const f32x4_any*)(z0 + j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[u * 4 + e] = v[e];
+      } else {
+        const u16x8_any v = *(const u16x8_any*)(z0 + j);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[u * 8 + e] = __uint_as_float((uint32_t)v[e] << 16);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < P; ++e) z[u * P + e] = j + e < j1 ? to_f32<T>(z0[j + e]) : -INFINITY;
+    }
   }
-  const T* z = (const T*)a.logits + (size_t)(before + i) * V;
-  float m = -INFINITY;
-  for (int j = tid; j < V; j += 256) m = fmaxf(m, to_f32<T>(z[j]));
+  float zmax = -INFINITY;                               // (of NaN alone: no maximum)
+#pragma unroll
+  for (int e = 0; e < E; ++e) zmax = fmaxf(zmax, z[e]);
+  float m = zmax;
+#pragma unroll
   for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-  if ((tid & 63) == 0) s_f[tid >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(s_f[0], s_f[1]), fmaxf(s_f[2], s_f[3]));
-  float sum = 0.f, sy = 0.f;
-  for (int j = tid; j < V; j += 256) {
-    const float x = to_f32<T>(z[j]);
-    if (x == -INFINITY) continue;
-    const float y = (x - m) * a.inv_temp, e = expf(y);
-    sum += e;
-    if (e != 0.f) sy += e * y;
+  const float c = a.inv_temp * 1.44269504088896341f, m0 = m == -INFINITY ? 0.f : m;
+  float sum = 0.f, q = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float t = (z[e] - m0) * c, x = __builtin_amdgcn_exp2f(t);           // (m c - z c would overflow where logits are near the type's lowest value)
+    sum += x;
+    q += x * fmaxf(t, -1e4f);                           // a masked one: 0 * -1e4
   }
-  for (int o = 1; o < 64; o <<= 1) { sum += __shfl_xor(sum, o); sy += __shfl_xor(sy, o); }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) { sum += __shfl_xor(sum, o); q += __shfl_xor(q, o); }
+  if (lane == 0) s_stats[wave] = Stats{m, sum, q};
+  int n_found = 0;
+  if constexpr (TOP)
+    n_found = select_top<E>(z, zmax, a.n_top, [&](int e) { return j0 + (e / P * kThreads + tid) * P + e % P; },
+                            [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
   __syncthreads();
-  if ((tid & 63) == 0) { s_f[4 + (tid >> 6)] = sum; s_f[8 + (tid >> 6)] = sy; }
-  __syncthreads();
-  sum = s_f[4] + s_f[5] + s_f[6] + s_f[7];
-  sy = s_f[8] + s_f[9] + s_f[10] + s_f[11];
-  const bool empty = m == -INFINITY && sum == 0.f;
-  const float lse = logf(sum);
-  auto logp = [&](float x) { return empty || x == -INFINITY ? -INFINITY : (x - m) * a.inv_temp - lse; };
+  Stats st = s_stats[0];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) st = merge_stats(st, s_stats[w], c);
+
+  if (segs > 1) {
+    const wt_buf bp = wt_buffer(part + (size_t)entry * segs), bt = wt_buffer(part_top + (size_t)entry * segs * a.n_top);
+    if (tid == 0) wt_store4(bp, sg * 16, wt_f32x4{st.m, st.s, st.q, 0.f});
+    if constexpr (TOP)
+      for (int r = tid; r < a.n_top; r += kThreads) {
+        const bool is = r < n_found;
+        wt_store2(bt, (sg * a.n_top + r) * 8, is ? s_top[r].z : -INFINITY, __int_as_float(is ? s_top[r].j : 0x7fffffff));
+      }
+    if (!publish_arrival(counters + entry, segs, &s_flag)) return;
+    // the last segment of the row: all of them, in their order
+    if (tid < segs) {
+      const wt_f32x4 p = wt_load4(bp, tid * 16);
+      s_sel.list[tid * 2] = Top{p[0], __float_as_int(p[1])};
+      s_sel.list[tid * 2 + 1] = Top{p[2], 0};
+    }
+    float tz[kMergeEach];
+    int tj[kMergeEach];
+    float tmax = -INFINITY;
+    if constexpr (TOP) {
+#pragma unroll
+      for (int e = 0; e < kMergeEach; ++e) {
+        const int i = e * kThreads + tid;
+        wt_f32x2 p{-INFINITY, 0.f};
+        if (i < segs * a.n_top) p = wt_load2(bt, i * 8);
+        tz[e] = p[0];
+        tj[e] = __float_as_int(p[1]);
+        tmax = fmaxf(tmax, tz[e]);
+      }
+    }
+    __syncthreads();
+    st = Stats{s_sel.list[0].z, __int_as_float(s_sel.list[0].j), s_sel.list[1].z};
+    for (int g = 1; g < segs; ++g) st = merge_stats(st, Stats{s_sel.list[2 * g].z, __int_as_float(s_sel.list[2 * g].j), s_sel.list[2 * g + 1].z}, c);
+    __syncthreads();                                    // the list is used again
+    if constexpr (TOP) {
+      n_found = select_top<kMergeEach>(tz, tmax, a.n_top, [&](int e) { return tj[e]; }, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
+      __syncthreads();
+    }
+  }
+  const bool empty = st.m == -INFINITY && st.s == 0.f;
+  const float lse = logf(st.s), ln2 = 0.693147180559945309f;
+  auto logp = [&](float x) { return st.s != st.s ? st.s : empty || x == -INFINITY ? -INFINITY : (x - st.m) * a.inv_temp - lse; };
   if (tid == 0) {
-    a.logprob[at] = sum != sum ? sum : logp(to_f32<T>(z[tok]));
-    if (a.entropy) a.entropy[at] = empty ? 0.f : lse - sy / sum;
+    a.logprob[entry] = logp(z_tok);
+    if (a.entropy) a.entropy[entry] = empty ? 0.f : lse - st.q * ln2 / st.s;
   }
-  unsigned long long last = ~0ull;
-  for (int j = 0; j < a.n_top; ++j) {                  // the largest key below the last one
-    unsigned long long best = 0;
-    for (int x = tid; x < V; x += 256) {
-      const unsigned long long key = logprob_key(to_f32<T>(z[x]), x);
-      if (key < last && key > best) best = key;
+  if constexpr (TOP)
+    for (int r = tid; r < a.n_top; r += kThreads) {
+      const bool is = r < n_found;
+      a.top_tokens[(size_t)entry * a.n_top + r] = is ? s_top[r].j : -1;
+      a.top_logprobs[(size_t)entry * a.n_top + r] = is ? logp(s_top[r].z) : -INFINITY;
     }
-    for (int o = 1; o < 64; o <<= 1) { const unsigned long long y = __shfl_xor(best, o); best = y > best ? y : best; }
-    __syncthreads();
-    if ((tid & 63) == 0) s_u[tid >> 6] = best;
-    __syncthreads();
-    for (int w = 0; w < 4; ++w) best = s_u[w] > best ? s_u[w] : best;
-    last = best;
-    if (tid == 0) {
-      const int x = best ? (int)(0xffffffffu - (uint32_t)best) : -1;
-      a.top_tokens[at * a.n_top + j] = x;
-      a.top_logprobs[at * a.n_top + j] = x < 0 ? -INFINITY : sum != sum ? sum : logp(to_f32<T>(z[x]));
-    }
-  }
+}
+
+// Segments of a row: as long as the registers of a workgroup take (64 elements a thread), shorter where there are few rows.
+struct Cutting { int seg, segs; };
+constexpr int kSegMost = kThreads * 64, kSegLeast = 4096, kWanted = 1024;
+Cutting cut_rows(long long rows, int vocab) {
+  const int least = (vocab + kSegMost - 1) / kSegMost, most = (vocab + kSegLeast - 1) / kSegLeast;
+  const long long want = (kWanted + rows - 1) / rows;
+  int segs = want < least ? least : want > most ? most : (int)want;
+  if (segs > kMaxSegs) segs = kMaxSegs;                 // (never fewer than `least`: kLogprobMaxVocab)
+  const int seg = ((vocab + segs - 1) / segs + 7) / 8 * 8;
+  return Cutting{seg, (vocab + seg - 1) / seg};
 }
 }  // namespace
 
-size_t logprob_workspace(int, int, int, int) { return 256; }
+size_t logprob_workspace(int B, int k_max, int vocab, int n_top) {
+  const long long rows = (long long)B * (k_max + 1), least = (vocab + kSegMost - 1) / kSegMost;
+  const long long parts = rows * least > kWanted + rows ? rows * least : kWanted + rows;   // of this many rows or of fewer
+  return (size_t)kLogprobMaxRows * sizeof(int32_t) + parts * (sizeof(wt_f32x4) + (size_t)n_top * sizeof(Top)) + 256;
+}
 
-void launch_logprob(const LogprobArgs& a, int B, int dtype, void*, hipStream_t st) {
-  const dim3 grid(B * (a.k_max + 1));
-  if (dtype == BS_F32) hipLaunchKernelGGL(logprob_kernel<float>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(logprob_kernel<bf16>, grid, dim3(256), 0, st, a);
+void launch_logprob(const LogprobArgs& a, int B, int dtype, void* workspace, hipStream_t st) {
+  const long long rows = (long long)B * (a.k_max + 1);
+  const Cutting cut = cut_rows(rows, a.vocab);
+  int32_t* counters = (int32_t*)workspace;
+  wt_f32x4* part = (wt_f32x4*)(counters + kLogprobMaxRows);
+  Top* part_top = (Top*)(part + rows * cut.segs);
+  const dim3 grid((unsigned)(rows * cut.segs));
+#define BS_LOGPROB(T_, TOP_) hipLaunchKernelGGL((logprob_kernel<T_, TOP_>), grid, dim3(kThreads), 0, st, a, cut.seg, cut.segs, part, part_top, counters)
+  if (dtype == BS_F32) { if (a.n_top > 0) BS_LOGPROB(float, true); else BS_LOGPROB(float, false); }
+  else { if (a.n_top > 0) BS_LOGPROB(bf16, true); else BS_LOGPROB(bf16, false); }
+#undef BS_LOGPROB
 }
