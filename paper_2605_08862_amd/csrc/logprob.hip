@@ -15,9 +15,33 @@ constexpr int kThreads = 256, kVecs = 16, kList = 512;  // vectors of sixteen by
 constexpr int kMaxSegs = kLogprobMaxVocab / (kThreads * 64);
 constexpr int kMergeEach = kMaxSegs * kLogprobMaxTop / kThreads;     // list entries of a thread in the merge
 
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint16_t u16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <typename T> constexpr int kPer = 16 / sizeof(T);                    // elements of a vector
+template <typename T> struct Vec;                                            // a vector that starts on any element
+template <> struct Vec<float> { typedef uint32_t V __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct Vec<bf16> { typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2))); };
+// element e of a vector
+template <typename T> __device__ __forceinline__ float element(const u32x4& v, int e);
+template <> __device__ __forceinline__ float element<float>(const u32x4& v, int e) { return __uint_as_float(v[e]); }
+template <> __device__ __forceinline__ float element<bf16>(const u32x4& v, int e) { return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16); }
+
+// Over the 64 lanes, in registers: neighbours, halves of rows of sixteen lanes, then the rows.
+template <int CTRL> __device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true)); }
+template <typename F> __device__ __forceinline__ float wave_reduce(float v, const F& f) {
+  v = f(v, dpp<0xB1>(v));                               // quad_perm 1 0 3 2
+  v = f(v, dpp<0x4E>(v));                               // quad_perm 2 3 0 1
+  v = f(v, dpp<0x141>(v));                              // row_half_mirror
+  v = f(v, dpp<0x140>(v));                              // row_mirror
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+#endif
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) { return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float wave_sum(float v) { return wave_reduce(v, [](float a, float b) { return a + b; }); }
 
 struct Top { float z; int j; };
 __device__ __forceinline__ bool better(float za, int ja, float zb, int jb) { return za > zb || (za == zb && ja < jb); }
@@ -25,55 +49,62 @@ __device__ __forceinline__ bool better(float za, int ja, float zb, int jb) { ret
 struct SelectShared {
   float group[4][64];
   Top list[kList];
+  int rank[kList];
   int n;
   Top best[4];
 };
 
-// The n best of the elements that the threads hold in z (E each, their indexes by `index`), -inf and NaN are none.  out(rank, z, j) is called once for every
-// rank that is taken; returns how many are.  zmax: largest z of the thread.
-template <int E, typename Index, typename Out>
-__device__ __forceinline__ int select_top(const float (&z)[E], float zmax, int n, const Index& index, const Out& out, SelectShared& s) {
+// The n best of the elements that the threads have, E each; load(thread, e) gives an element of any thread and its index (a thread reads others' too, 64 at a
+// time: E is a multiple of 64 or less than that); -inf and NaN are none.  out(rank, z, j) is called once for every rank that is taken; returns how many are.
+// zmax: the thread's largest.
+template <int E, typename Load, typename Out>
+__device__ __forceinline__ int select_top(float zmax, int n, const Load& load, const Out& out, SelectShared& s) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   s.group[wave][lane] = zmax;
   if (tid == 0) s.n = 0;
   __syncthreads();
-  // bound: the n-th largest of the 64 groups (a lane of all four waves); equal ones in the order of the lanes
-  const float g = fmaxf(fmaxf(s.group[0][lane], s.group[1][lane]), fmaxf(s.group[2][lane], s.group[3][lane]));
-  int before = 0;
+  // bound: no larger than the n-th largest of 64 groups (a lane of all four waves), off by less than 2^-7 of it: the first sixteen bits of its ranking key
+  const uint32_t g = filter_key(fmaxf(fmaxf(s.group[0][lane], s.group[1][lane]), fmaxf(s.group[2][lane], s.group[3][lane])));
+  uint32_t key = 0;
 #pragma unroll
-  for (int o = 0; o < 64; ++o) {
-    const float x = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), o));
-    before += x > g || (x == g && o < lane) ? 1 : 0;
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t t = key | 1u << bit;
+    if (__popcll(__ballot(g >= t)) >= n) key = t;
   }
-  const unsigned long long at = __ballot(before == n - 1);
-  const float bound = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), __ffsll((long long)at) - 1));
-  if (__any(zmax >= bound && zmax > -INFINITY)) {
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (z[e] >= bound && z[e] > -INFINITY) {
+  const float bound = key <= 0x007fffffu ? -INFINITY : __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+  // the few threads that have a candidate, one after the other: their elements are read again, one by each lane
+  for (unsigned long long have = __ballot(zmax >= bound && zmax > -INFINITY); have; have &= have - 1) {
+    const int owner = wave * 64 + __ffsll((long long)have) - 1;
+    for (int e0 = 0; e0 < E; e0 += 64) {
+      if (e0 + lane >= E) continue;
+      const Top t = load(owner, e0 + lane);
+      if (t.z >= bound && t.z > -INFINITY) {
         const int k = atomicAdd(&s.n, 1);
-        if (k < kList) s.list[k] = Top{z[e], index(e)};
+        if (k < kList) { s.list[k] = t; s.rank[k] = 0; }
       }
+    }
   }
   __syncthreads();
   const int found = s.n;
-  if (found <= kList) {
-    for (int k = tid; k < found; k += kThreads) {
+  if (found <= kList) {                                 // a wave counts against a quarter of the list
+    const int o0 = found * wave / 4, o1 = found * (wave + 1) / 4;
+    for (int k = lane; k < found; k += 64) {
       const Top t = s.list[k];
       int rank = 0;
-      for (int o = 0; o < found; ++o) { const Top x = s.list[o]; rank += better(x.z, x.j, t.z, t.j) ? 1 : 0; }
-      if (rank < n) out(rank, t.z, t.j);
+      for (int o = o0; o < o1; ++o) { const Top x = s.list[o]; rank += better(x.z, x.j, t.z, t.j) ? 1 : 0; }
+      if (rank) atomicAdd(&s.rank[k], rank);
     }
+    __syncthreads();
+    for (int k = tid; k < found; k += kThreads) if (s.rank[k] < n) out(s.rank[k], s.list[k].z, s.list[k].j);
     return min(found, n);
   }
   // more than the list holds reach the bound (a segment of equal logits, say): one after the other
   Top last{INFINITY, -1};
   for (int r = 0; r < n; ++r) {
     Top best{-INFINITY, 0x7fffffff};
-#pragma unroll
     for (int e = 0; e < E; ++e) {
-      const int j = index(e);
-      if (better(last.z, last.j, z[e], j) && better(z[e], j, best.z, best.j)) best = Top{z[e], j};
+      const Top t = load(tid, e);
+      if (better(last.z, last.j, t.z, t.j) && better(t.z, t.j, best.z, best.j)) best = t;
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -141,8 +172,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(LogprobArgs a, int se
   __shared__ Stats s_stats[4];
   __shared__ Top s_top[kLogprobMaxTop];
   __shared__ int s_i[4], s_flag;
-  constexpr int P = kPer<T>, E = kVecs * (P > 4 ? 4 : P);                     // elements of a thread: 64 whatever the type
-  constexpr int NV = E / P;                                                  // vectors
+  constexpr int P = kPer<T>, E = kVecs * P;             // elements of a vector, of a thread
   const int entry = blockIdx.x / segs, sg = blockIdx.x - entry * segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.vocab;
   size_t row;
   int tok;
@@ -152,49 +182,51 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(LogprobArgs a, int se
   const float z_tok = to_f32<T>(z0[tok]);
 
   // ---- the segment: element e of a thread is j0 + (e / P * kThreads + tid) * P + e % P
-  float z[E];
+  u32x4 v[kVecs];
+  const uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;           // -inf
 #pragma unroll
-  for (int u = 0; u < NV; ++u) {
+  for (int u = 0; u < kVecs; ++u) {
     const int j = j0 + (u * kThreads + tid) * P;
-    if (j0 + u * kThreads * P >= j1) {                  // the same for all threads
-#pragma unroll
-      for (int e = 0; e < P; ++e) z[u * P + e] = -INFINITY;
-    } else if (j + P <= j1) {
-      if constexpr (P == 4) {
-        const f32x4_any v = *(const f32x4_any*)(z0 + j);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) z[u * 4 + e] = v[e];
-      } else {
-        const u16x8_any v = *(const u16x8_any*)(z0 + j);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) z[u * 8 + e] = __uint_as_float((uint32_t)v[e] << 16);
-      }
+    v[u] = u32x4{none, none, none, none};
+    if (j0 + u * kThreads * P >= j1) continue;          // the same for all threads
+    if (j + P <= j1) {
+      v[u] = *(const typename Vec<T>::V*)(z0 + j);
     } else {
 #pragma unroll
-      for (int e = 0; e < P; ++e) z[u * P + e] = j + e < j1 ? to_f32<T>(z0[j + e]) : -INFINITY;
+      for (int e = 0; e < P; ++e)
+        if (j + e < j1) {
+          if constexpr (P == 4) v[u][e] = ((const uint32_t*)z0)[j + e];
+          else v[u][e / 2] = e & 1 ? (v[u][e / 2] & 0xffffu) | (uint32_t)((const uint16_t*)z0)[j + e] << 16 : (v[u][e / 2] & 0xffff0000u) | ((const uint16_t*)z0)[j + e];
+        }
     }
   }
   float zmax = -INFINITY;                               // (of NaN alone: no maximum)
 #pragma unroll
-  for (int e = 0; e < E; ++e) zmax = fmaxf(zmax, z[e]);
-  float m = zmax;
+  for (int u = 0; u < kVecs; ++u)
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+    for (int e = 0; e < P; ++e) zmax = fmaxf(zmax, element<T>(v[u], e));
+  const float m = wave_max(zmax);
   const float c = a.inv_temp * 1.44269504088896341f, m0 = m == -INFINITY ? 0.f : m;
   float sum = 0.f, q = 0.f;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const float t = (z[e] - m0) * c, x = __builtin_amdgcn_exp2f(t);           // (m c - z c would overflow where logits are near the type's lowest value)
-    sum += x;
-    q += x * fmaxf(t, -1e4f);                           // a masked one: 0 * -1e4
-  }
+  for (int u = 0; u < kVecs; ++u) {
+    if (j0 + u * kThreads * P >= j1) break;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) { sum += __shfl_xor(sum, o); q += __shfl_xor(q, o); }
+    for (int e = 0; e < P; ++e) {
+      const float t = (element<T>(v[u], e) - m0) * c, x = __builtin_amdgcn_exp2f(t);      // (m c - z c would overflow where logits are near the type's lowest value)
+      sum += x;
+      q += x * fmaxf(t, -1e4f);                         // a masked one: 0 * -1e4
+    }
+  }
+  sum = wave_sum(sum);
+  q = wave_sum(q);
   if (lane == 0) s_stats[wave] = Stats{m, sum, q};
   int n_found = 0;
   if constexpr (TOP)
-    n_found = select_top<E>(z, zmax, a.n_top, [&](int e) { return j0 + (e / P * kThreads + tid) * P + e % P; },
-                            [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
+    n_found = select_top<E>(zmax, a.n_top, [&](int thread, int e) {
+                              const int j = j0 + (e / P * kThreads + thread) * P + e % P;
+                              return j < j1 ? Top{to_f32<T>(z0[j]), j} : Top{-INFINITY, j};
+                            }, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
   __syncthreads();
   Stats st = s_stats[0];
 #pragma unroll
@@ -215,26 +247,21 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(LogprobArgs a, int se
       s_sel.list[tid * 2] = Top{p[0], __float_as_int(p[1])};
       s_sel.list[tid * 2 + 1] = Top{p[2], 0};
     }
-    float tz[kMergeEach];
-    int tj[kMergeEach];
+    auto entry_of = [&](int thread, int e) {
+      const int i = e * kThreads + thread;
+      if (i >= segs * a.n_top) return Top{-INFINITY, 0x7fffffff};
+      const wt_f32x2 p = wt_load2(bt, i * 8);
+      return Top{p[0], __float_as_int(p[1])};
+    };
     float tmax = -INFINITY;
-    if constexpr (TOP) {
-#pragma unroll
-      for (int e = 0; e < kMergeEach; ++e) {
-        const int i = e * kThreads + tid;
-        wt_f32x2 p{-INFINITY, 0.f};
-        if (i < segs * a.n_top) p = wt_load2(bt, i * 8);
-        tz[e] = p[0];
-        tj[e] = __float_as_int(p[1]);
-        tmax = fmaxf(tmax, tz[e]);
-      }
-    }
+    if constexpr (TOP)
+      for (int e = 0; e * kThreads < segs * a.n_top; ++e) tmax = fmaxf(tmax, entry_of(tid, e).z);
     __syncthreads();
     st = Stats{s_sel.list[0].z, __int_as_float(s_sel.list[0].j), s_sel.list[1].z};
     for (int g = 1; g < segs; ++g) st = merge_stats(st, Stats{s_sel.list[2 * g].z, __int_as_float(s_sel.list[2 * g].j), s_sel.list[2 * g + 1].z}, c);
     __syncthreads();                                    // the list is used again
     if constexpr (TOP) {
-      n_found = select_top<kMergeEach>(tz, tmax, a.n_top, [&](int e) { return tj[e]; }, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
+      n_found = select_top<kMergeEach>(tmax, a.n_top, entry_of, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
       __syncthreads();
     }
   }
@@ -253,11 +280,11 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(LogprobArgs a, int se
     }
 }
 
-// Segments of a row: as long as the registers of a workgroup take (64 elements a thread), shorter where there are few rows.
+// Segments of a row: as long as the registers of a workgroup take (kVecs vectors a thread), shorter where there are few rows.
 struct Cutting { int seg, segs; };
-constexpr int kSegMost = kThreads * 64, kSegLeast = 4096, kWanted = 1024;
-Cutting cut_rows(long long rows, int vocab) {
-  const int least = (vocab + kSegMost - 1) / kSegMost, most = (vocab + kSegLeast - 1) / kSegLeast;
+constexpr int kSegLeast = 4096, kWanted = 1024;
+Cutting cut_rows(long long rows, int vocab, int per) {
+  const int longest = kThreads * kVecs * per, least = (vocab + longest - 1) / longest, most = (vocab + kSegLeast - 1) / kSegLeast;
   const long long want = (kWanted + rows - 1) / rows;
   int segs = want < least ? least : want > most ? most : (int)want;
   if (segs > kMaxSegs) segs = kMaxSegs;                 // (never fewer than `least`: kLogprobMaxVocab)
@@ -267,14 +294,14 @@ Cutting cut_rows(long long rows, int vocab) {
 }  // namespace
 
 size_t logprob_workspace(int B, int k_max, int vocab, int n_top) {
-  const long long rows = (long long)B * (k_max + 1), least = (vocab + kSegMost - 1) / kSegMost;
+  const long long rows = (long long)B * (k_max + 1), least = (vocab + kThreads * kVecs * kPer<float> - 1) / (kThreads * kVecs * kPer<float>);
   const long long parts = rows * least > kWanted + rows ? rows * least : kWanted + rows;   // of this many rows or of fewer
   return (size_t)kLogprobMaxRows * sizeof(int32_t) + parts * (sizeof(wt_f32x4) + (size_t)n_top * sizeof(Top)) + 256;
 }
 
 void launch_logprob(const LogprobArgs& a, int B, int dtype, void* workspace, hipStream_t st) {
   const long long rows = (long long)B * (a.k_max + 1);
-  const Cutting cut = cut_rows(rows, a.vocab);
+  const Cutting cut = cut_rows(rows, a.vocab, dtype == BS_F32 ? kPer<float> : kPer<bf16>);
   int32_t* counters = (int32_t*)workspace;
   wt_f32x4* part = (wt_f32x4*)(counters + kLogprobMaxRows);
   Top* part_top = (Top*)(part + rows * cut.segs);
