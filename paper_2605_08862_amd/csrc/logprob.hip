@@ -43,22 +43,33 @@ template <typename F> __device__ __forceinline__ float wave_reduce(float v, cons
 __device__ __forceinline__ float wave_max(float v) { return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float wave_sum(float v) { return wave_reduce(v, [](float a, float b) { return a + b; }); }
 
+// What a lane wrote to LDS, others of its wave read behind this.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 struct Top { float z; int j; };
 __device__ __forceinline__ bool better(float za, int ja, float zb, int jb) { return za > zb || (za == zb && ja < jb); }
 
+constexpr int kOwners = 4;                              // threads of a wave whose elements are looked at together
 struct SelectShared {
   float group[4][64];
+  union {
+    u32x4 stage[4][kOwners][kVecs];                     // elements of those threads
+    Top parts[kMaxSegs * kLogprobMaxTop];               // merge: the segments' alternatives
+  };
   Top list[kList];
   int rank[kList];
   int n;
   Top best[4];
 };
 
-// The n best of the elements that the threads have, E each; load(thread, e) gives an element of any thread and its index (a thread reads others' too, 64 at a
-// time: E is a multiple of 64 or less than that); -inf and NaN are none.  out(rank, z, j) is called once for every rank that is taken; returns how many are.
-// zmax: the thread's largest.
-template <int E, typename Load, typename Out>
-__device__ __forceinline__ int select_top(float zmax, int n, const Load& load, const Out& out, SelectShared& s) {
+// The n best of the elements that the threads have, E each; -inf and NaN are none.  zmax: the thread's largest.  src.show(p): called by the threads with a
+// candidate, up to kOwners of a wave, puts the thread's elements in place p; src.seen(p, owner, e): element e of the thread `owner` shown in place p; src.own(e):
+// of the calling thread.  out(rank, z, j) is called once for every rank that is taken; returns how many are.
+template <int E, typename Source, typename Out>
+__device__ __forceinline__ int select_top(float zmax, int n, const Source& src, const Out& out, SelectShared& s) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   s.group[wave][lane] = zmax;
   if (tid == 0) s.n = 0;
@@ -72,17 +83,27 @@ __device__ __forceinline__ int select_top(float zmax, int n, const Load& load, c
     if (__popcll(__ballot(g >= t)) >= n) key = t;
   }
   const float bound = key <= 0x007fffffu ? -INFINITY : __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
-  // the few threads that have a candidate, one after the other: their elements are read again, one by each lane
-  for (unsigned long long have = __ballot(zmax >= bound && zmax > -INFINITY); have; have &= have - 1) {
-    const int owner = wave * 64 + __ffsll((long long)have) - 1;
-    for (int e0 = 0; e0 < E; e0 += 64) {
-      if (e0 + lane >= E) continue;
-      const Top t = load(owner, e0 + lane);
-      if (t.z >= bound && t.z > -INFINITY) {
-        const int k = atomicAdd(&s.n, 1);
-        if (k < kList) { s.list[k] = t; s.rank[k] = 0; }
+  // the elements of the few threads that have a candidate, one by each lane
+  for (unsigned long long have = __ballot(zmax >= bound && zmax > -INFINITY); have;) {
+    const int p = __popcll(have & ((1ull << lane) - 1));
+    if ((have >> lane & 1) && p < kOwners) src.show(p);
+    wave_fence();
+#pragma unroll
+    for (int p = 0; p < kOwners; ++p) {
+      if (!have) break;
+      const int owner = wave * 64 + __ffsll((long long)have) - 1;
+      have &= have - 1;
+#pragma unroll
+      for (int e0 = 0; e0 < E; e0 += 64) {
+        if (e0 + lane >= E) continue;
+        const Top t = src.seen(p, owner, e0 + lane);
+        if (t.z >= bound && t.z > -INFINITY) {
+          const int k = atomicAdd(&s.n, 1);
+          if (k < kList) { s.list[k] = t; s.rank[k] = 0; }
+        }
       }
     }
+    wave_fence();
   }
   __syncthreads();
   const int found = s.n;
@@ -103,7 +124,7 @@ __device__ __forceinline__ int select_top(float zmax, int n, const Load& load, c
   for (int r = 0; r < n; ++r) {
     Top best{-INFINITY, 0x7fffffff};
     for (int e = 0; e < E; ++e) {
-      const Top t = load(tid, e);
+      const Top t = src.own(e);
       if (better(last.z, last.j, t.z, t.j) && better(t.z, t.j, best.z, best.j)) best = t;
     }
 #pragma unroll
@@ -122,6 +143,35 @@ __device__ __forceinline__ int select_top(float zmax, int n, const Load& load, c
   }
   return n;
 }
+
+// A segment: element e of a thread is j0 + (e / P * kThreads + thread) * P + e % P, in vector e / P.
+template <typename T> struct SegmentSource {
+  const u32x4 (&v)[kVecs];
+  const T* z0;
+  int j0, j1;
+  SelectShared& s;
+  __device__ __forceinline__ int index(int thread, int e) const { return j0 + (e / kPer<T> * kThreads + thread) * kPer<T> + e % kPer<T>; }
+  __device__ __forceinline__ void show(int p) const {
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) s.stage[threadIdx.x >> 6][p][u] = v[u];
+  }
+  __device__ __forceinline__ Top seen(int p, int owner, int e) const {
+    return Top{to_f32<T>(((const T*)s.stage[threadIdx.x >> 6][p])[e]), index(owner, e)};
+  }
+  __device__ __forceinline__ Top own(int e) const {
+    const int j = index(threadIdx.x, e);
+    return Top{j < j1 ? to_f32<T>(z0[j]) : -INFINITY, j};
+  }
+};
+// The alternatives of a row's segments, in LDS.
+struct PartsSource {
+  int n;
+  SelectShared& s;
+  __device__ __forceinline__ Top at(int i) const { return i < n ? s.parts[i] : Top{-INFINITY, 0x7fffffff}; }
+  __device__ __forceinline__ void show(int) const {}
+  __device__ __forceinline__ Top seen(int, int owner, int e) const { return at(e * kThreads + owner); }
+  __device__ __forceinline__ Top own(int e) const { return at(e * kThreads + threadIdx.x); }
+};
 
 // Maximum and sums of a part of a row, in units of log2: t = (z - m) c with c = log2(e) / T;  s = sum 2^t, q = sum 2^t t.
 struct Stats { float m, s, q; };
@@ -206,6 +256,10 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(LogprobArgs a, int se
 #pragma unroll
     for (int e = 0; e < P; ++e) zmax = fmaxf(zmax, element<T>(v[u], e));
   const float m = wave_max(zmax);
+  if constexpr (P == 8) {                               // unpacked again below: kept, the elements would take 128 registers
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) asm volatile("" : "+v"(v[u]));
+  }
   const float c = a.inv_temp * 1.44269504088896341f, m0 = m == -INFINITY ? 0.f : m;
   float sum = 0.f, q = 0.f;
 #pragma unroll
@@ -223,10 +277,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(LogprobArgs a, int se
   if (lane == 0) s_stats[wave] = Stats{m, sum, q};
   int n_found = 0;
   if constexpr (TOP)
-    n_found = select_top<E>(zmax, a.n_top, [&](int thread, int e) {
-                              const int j = j0 + (e / P * kThreads + thread) * P + e % P;
-                              return j < j1 ? Top{to_f32<T>(z0[j]), j} : Top{-INFINITY, j};
-                            }, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
+    n_found = select_top<E>(zmax, a.n_top, SegmentSource<T>{v, z0, j0, j1, s_sel}, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
   __syncthreads();
   Stats st = s_stats[0];
 #pragma unroll
@@ -247,21 +298,21 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(LogprobArgs a, int se
       s_sel.list[tid * 2] = Top{p[0], __float_as_int(p[1])};
       s_sel.list[tid * 2 + 1] = Top{p[2], 0};
     }
-    auto entry_of = [&](int thread, int e) {
-      const int i = e * kThreads + thread;
-      if (i >= segs * a.n_top) return Top{-INFINITY, 0x7fffffff};
-      const wt_f32x2 p = wt_load2(bt, i * 8);
-      return Top{p[0], __float_as_int(p[1])};
-    };
     float tmax = -INFINITY;
-    if constexpr (TOP)
-      for (int e = 0; e * kThreads < segs * a.n_top; ++e) tmax = fmaxf(tmax, entry_of(tid, e).z);
+    if constexpr (TOP) {
+      const int n = segs * a.n_top;
+      for (int i = tid; i < n; i += kThreads) {
+        const wt_f32x2 p = wt_load2(bt, i * 8);
+        s_sel.parts[i] = Top{p[0], __float_as_int(p[1])};
+        tmax = fmaxf(tmax, p[0]);
+      }
+    }
     __syncthreads();
     st = Stats{s_sel.list[0].z, __int_as_float(s_sel.list[0].j), s_sel.list[1].z};
     for (int g = 1; g < segs; ++g) st = merge_stats(st, Stats{s_sel.list[2 * g].z, __int_as_float(s_sel.list[2 * g].j), s_sel.list[2 * g + 1].z}, c);
     __syncthreads();                                    // the list is used again
     if constexpr (TOP) {
-      n_found = select_top<kMergeEach>(tmax, a.n_top, entry_of, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
+      n_found = select_top<kMergeEach>(tmax, a.n_top, PartsSource{segs * a.n_top, s_sel}, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
       __syncthreads();
     }
   }
