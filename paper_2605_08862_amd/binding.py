@@ -20,7 +20,7 @@ EXPORTS = ["bs_workspace_bytes", "bs_create", "bs_destroy", "bs_last_error", "bs
            "bs_verify_step", "bs_accept_resample", "bs_accept_resample_logits", "bs_kv_commit", "bs_kv_write",
            "bs_kv_read", "bs_poll_status", "bs_profile_begin", "bs_profile_end", "bs_index_build", "bs_index_free",
            "bs_index_bind", "bs_set_filter", "bs_kv_lengths", "bs_accept_resample_logits_noalloc", "bs_kvq_write", "bs_kvq_read",
-           "bs_kvq_workspace_bytes", "bs_kvq_attention", "bs_token_logprobs_workspace_bytes", "bs_token_logprobs"]
+           "bs_kvq_workspace_bytes", "bs_kvq_attention", "bs_kvq_bind_bytes", "bs_kvq_bind", "bs_token_logprobs_workspace_bytes", "bs_token_logprobs"]
 PROF_CLASSES = {"attention": 1, "gemm_qkv": 2, "gemm_o": 3, "gemm_gate_up": 4, "gemm_down": 5, "lmhead": 6,
                 "sample": 7, "lookup": 8, "empty": 9}
 
@@ -95,11 +95,14 @@ def lib():
         L.bs_kvq_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.bs_kvq_workspace_bytes.restype = C.c_size_t
         L.bs_kvq_attention.argtypes = [vp, i32, vp, vp, vp, i32, i32, vp, C.c_int64, vp, vp, vp, C.c_size_t, vp]
+        L.bs_kvq_bind_bytes.argtypes = [vp]
+        L.bs_kvq_bind_bytes.restype = C.c_size_t
+        L.bs_kvq_bind.argtypes = [vp, vp, vp, C.c_size_t]
         L.bs_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.bs_token_logprobs_workspace_bytes.restype = C.c_size_t
         L.bs_token_logprobs.argtypes = [i32, i32, vp, i32, vp, i32, vp, vp, f32, i32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
         for name in EXPORTS:
-            if name not in ("bs_kvq_workspace_bytes", "bs_token_logprobs_workspace_bytes", "bs_workspace_bytes", "bs_destroy", "bs_last_error", "bs_index_free"):
+            if name not in ("bs_kvq_workspace_bytes", "bs_kvq_bind_bytes", "bs_token_logprobs_workspace_bytes", "bs_workspace_bytes", "bs_destroy", "bs_last_error", "bs_index_free"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -334,6 +337,18 @@ def bs_kvq_attention(desc, B, seq_slot, ctx_len, q_len, q_max, n_q_heads, q, out
                                 _here(status, dev), _here(workspace, dev), workspace.numel() * workspace.element_size(), _stream())
     if st != BS_OK:
         raise BsError(st, "bs_kvq_attention")
+
+
+def bs_kvq_bind_bytes(ctx):
+    return lib().bs_kvq_bind_bytes(ctx)
+
+
+def bs_kvq_bind(ctx, descs, workspace):
+    """descs: list of bs_kvq_desc, one per layer (None unbinds)."""
+    if descs is None:
+        _check(ctx, lib().bs_kvq_bind(ctx, None, None, 0))
+        return
+    _check(ctx, lib().bs_kvq_bind(ctx, (bs_kvq_desc * len(descs))(*descs), _ptr(workspace), workspace.numel() * workspace.element_size()))
 
 
 def bs_token_logprobs_workspace_bytes(B, k_max, vocab, n_top):

@@ -53,6 +53,9 @@ struct bs_ctx {
   int top_k = 0;              // top-k / top-p filter of the target distribution (bs_set_filter); 0 / 1.0 = off
   float top_p = 1.0f;
   float* filter_logits = nullptr;   // bf16 models: caller's [M_max, V] float32 scratch for the filtered path
+  // 8-bit cache (bs_kvq_bind): one view per layer, staging pages of a step's rows, attention workspace
+  std::vector<KvqView> kvq;
+  void *kvq_k = nullptr, *kvq_v = nullptr, *kvq_ws = nullptr;
   bool unfused_qkv = false;   // test hook: QKV GEMM + separate rotary kernel instead of the fused kernel
   std::vector<hipEvent_t> prof_ev;     // pairs (start, stop), created on first use
   size_t prof_used = 0;
@@ -429,25 +432,39 @@ bs_status bs_verify_step(bs_ctx* c, int B, const int32_t* seq_slot, const int32_
   const Shape& s = c->s;
   const int M_max = B * (k_max + 1);
   const Plan& p = c->plan;
-  launch_plan(p, c->kv, B, k_max, s.V, seq_slot, last_token, draft_tokens, draft_len, true, attention_plan_params(s, B, k_max),
-              s.L, st);
+  const bool kvq = !c->kvq.empty();
+  KvView kv = c->kv;
+  kv.staged = kvq;
+  launch_plan(p, kv, B, k_max, s.V, seq_slot, last_token, draft_tokens, draft_len, true, kvq ? AttnPlan{} : attention_plan_params(s, B, k_max), s.L, st);
+  // 8-bit cache: the layer's rows from the staging pages, then attention over it
+  const KvqSeqs seqs{B, k_max + 1, 1, p.seq_slot, p.seq_c, p.seq_k, p.row_start, 0, 0};
+  auto kvq_append = [&](int l) {
+    ProfScope ps(c, BS_PROF_GEMM_QKV, st);
+    launch_kvq_write_staged(c->kvq[l], seqs, c->kvq_k, c->kvq_v, p.status, st);
+  };
+  auto kvq_attention = [&](int l, int out_ld) {
+    ProfScope ps(c, BS_PROF_ATTENTION, st);
+    launch_kvq_step_attention(c->kvq[l], seqs, s.Hq, c->q, c->attn_out, out_ld, p.status, c->kvq_ws, st);
+  };
   const bool skinny = c->fragments && skinny_applies(s, M_max) && !c->unfused_qkv;
   const StepRules rules = skinny ? StepRules{} : step_rules(s, M_max);
-  if (skinny) launch_skinny_embed(s, p, c->kv, c->embed, c->h, c->ssq, c->inv_freq, c->rope_cos, c->rope_sin, st);
-  else launch_embed(s, p, c->kv, M_max, rules, c->embed, c->h, c->inv_freq, c->rope_cos, c->rope_sin, st);
+  if (skinny) launch_skinny_embed(s, p, kv, c->embed, c->h, c->ssq, c->inv_freq, c->rope_cos, c->rope_sin, st);
+  else launch_embed(s, p, kv, M_max, rules, c->embed, c->h, c->inv_freq, c->rope_cos, c->rope_sin, st);
   const bool fused_qkv = qkv_rope_applies(s, M_max) && !c->unfused_qkv;
   const bool slab_mode = s.dtype == BS_BF16;   // float32 epilogues go through K-split slabs (see gemm.hip)
   SlabCount pending{0, 0};                      // slabs of the last residual projection not yet added to h
   for (int l = 0; l < s.L; ++l) {
+    void *const k_pages = kvq ? c->kvq_k : c->k_pages[l], *const v_pages = kvq ? c->kvq_v : c->v_pages[l];
     { ProfScope ps(c, BS_PROF_EMPTY, st); }
     ReadAhead ahead{nullptr, 0};
     if (s.dtype == BS_BF16) ahead = ReadAhead{c->wo[l], packed_weight_elems(s.d, s.Hq * s.D) * sizeof(uint16_t)};
     if (skinny) {
       { ProfScope ps(c, BS_PROF_GEMM_QKV, st);
         launch_skinny_qkv(s, p, M_max, c->h, c->ssq, l == 0 ? 1 : s.d / 32, c->attn_norm[l], c->wqkv[l], c->rope_cos, c->rope_sin,
-                          c->q, c->k_pages[l], c->v_pages[l], c->sk, st); }
-      launch_attention(s, p, c->kv, l, B, c->B_max, k_max, M_max, c->q, c->k_pages[l], c->v_pages[l], c->attn_out, kSkinnyRows,
-                       c->attn_scratch, ahead, c->prof_class == BS_PROF_ATTENTION ? (void*)c : nullptr, st);
+                          c->q, k_pages, v_pages, c->sk, st); }
+      if (kvq) { kvq_append(l); kvq_attention(l, kSkinnyRows); }
+      else launch_attention(s, p, c->kv, l, B, c->B_max, k_max, M_max, c->q, k_pages, v_pages, c->attn_out, kSkinnyRows,
+                            c->attn_scratch, ahead, c->prof_class == BS_PROF_ATTENTION ? (void*)c : nullptr, st);
       { ProfScope ps(c, BS_PROF_GEMM_O, st);
         launch_skinny_resid(s, p, M_max, s.Hq * s.D, c->attn_out, c->wo[l], c->h, c->ssq, c->sk, st); }
       { ProfScope ps(c, BS_PROF_GEMM_GATE_UP, st);
@@ -459,16 +476,16 @@ bs_status bs_verify_step(bs_ctx* c, int B, const int32_t* seq_slot, const int32_
     launch_rmsnorm(s, p, M_max, c->h, c->slabs, pending, c->attn_norm[l], c->a, st);
     if (fused_qkv) {
       ProfScope ps(c, BS_PROF_GEMM_QKV, st);
-      launch_qkv_rope(s, p, M_max, rules.qkv, c->a, c->wqkv[l], c->rope_cos, c->rope_sin, c->q, c->k_pages[l], c->v_pages[l], st);
+      launch_qkv_rope(s, p, M_max, rules.qkv, c->a, c->wqkv[l], c->rope_cos, c->rope_sin, c->q, k_pages, v_pages, st);
     } else {
       ProfScope ps(c, BS_PROF_GEMM_QKV, st);
       const SlabCount nq = launch_gemm(s.dtype, EPI_STORE_F32, p.n_rows, M_max, s.Nqkv(), s.d, c->a, c->wqkv[l],
                                        slab_mode ? (void*)c->slabs : (void*)c->qkv, p.status, st, rules.slab[SLAB_QKV]);
-      launch_rope_append(s, p, M_max, c->rope_cos, c->rope_sin, slab_mode ? c->slabs : c->qkv, nq, c->q,
-                         c->k_pages[l], c->v_pages[l], st);
+      launch_rope_append(s, p, M_max, c->rope_cos, c->rope_sin, slab_mode ? c->slabs : c->qkv, nq, c->q, k_pages, v_pages, st);
     }
-    launch_attention(s, p, c->kv, l, B, c->B_max, k_max, M_max, c->q, c->k_pages[l], c->v_pages[l], c->attn_out, M_max, c->attn_scratch, ahead,
-                     c->prof_class == BS_PROF_ATTENTION ? (void*)c : nullptr, st);
+    if (kvq) { kvq_append(l); kvq_attention(l, M_max); }
+    else launch_attention(s, p, c->kv, l, B, c->B_max, k_max, M_max, c->q, k_pages, v_pages, c->attn_out, M_max, c->attn_scratch, ahead,
+                          c->prof_class == BS_PROF_ATTENTION ? (void*)c : nullptr, st);
     { ProfScope ps(c, BS_PROF_GEMM_O, st);
       pending = launch_gemm(s.dtype, EPI_RESID_ADD, p.n_rows, M_max, s.d, s.Hq * s.D, c->attn_out, c->wo[l],
                             slab_mode ? (void*)c->slabs : (void*)c->h, p.status, st, rules.slab[SLAB_O]); }
@@ -628,6 +645,14 @@ static bs_status kv_copy(bs_ctx* c, int layer, int slot, int pos0, int n, void* 
   if (layer < 0 || layer >= c->s.L || slot < 0 || slot >= c->kv.n_slots || pos0 < 0 || n < 0)
     return fail(c, BS_ESHAPE, "bs_kv_write/read: layer, slot or range out of bounds");
   if ((long)pos0 + n > (long)c->kv.max_pages * kPage) return fail(c, BS_ECAPACITY, "bs_kv_write/read: beyond the slot's pages");
+  if (!c->kvq.empty()) {
+    if (n == 0) return BS_OK;
+    const KvqSeqs q{1, n, n, nullptr, nullptr, nullptr, nullptr, slot, pos0};
+    const size_t stride = (size_t)c->s.Hkv * c->s.D;
+    if (to_pages) launch_kvq_write(c->kvq[layer], q, k_rows, v_rows, stride, c->plan.status, (hipStream_t)stream);
+    else launch_kvq_read(c->kvq[layer], q, k_rows, v_rows, stride, c->plan.status, (hipStream_t)stream);
+    return check_hip(c);
+  }
   launch_kv_copy(c->s, c->kv, slot, pos0, n, c->k_pages[layer], c->v_pages[layer], k_rows, v_rows, to_pages,
                  c->plan.status, (hipStream_t)stream);
   return check_hip(c);
@@ -782,12 +807,55 @@ bs_status bs_kvq_attention(const bs_kvq_desc* kv, int B, const int32_t* seq_slot
   if (!kvq_heads_ok(n_q_heads, kv->n_kv_heads, kv->head_dim) || B < 1 || B > 4096 || q_max < 1 || (int64_t)q_max > (int64_t)kv->max_pages_per_seq * kPage ||
       q_stride < (int64_t)n_q_heads * kv->head_dim)
     return BS_ESHAPE;
-  // 38 for each step of 128 tokens at most, over all units, counted in 32 bits
-  if ((int64_t)B * kv->n_kv_heads * (kv->max_pages_per_seq / 2 + 1) > ((int64_t)1 << 25) / ((int64_t)q_max * (n_q_heads / kv->n_kv_heads) / 128 + 1)) return BS_ESHAPE;
+  if (!kvq_attention_counts(B, kv->n_kv_heads, n_q_heads / kv->n_kv_heads, kv->max_pages_per_seq, q_max)) return BS_ESHAPE;
   if (workspace_bytes < kvq_attention_workspace(n_q_heads, kv->n_kv_heads, kv->head_dim, q_max)) return BS_ECAPACITY;
   const KvqSeqs s{B, q_max, 0, seq_slot, ctx_len, q_len, nullptr, 0, 0};
   launch_kvq_attention(view_of(*kv), s, n_q_heads, q, (size_t)q_stride, out, status, workspace, (hipStream_t)stream);
   return last_hip();
+}
+
+namespace {
+// Staging pages of a step's K and V rows, then the attention workspace.
+size_t kvq_bind_carve(const bs_ctx* c, char* base, void** k, void** v, void** ws) {
+  Carver w{base};
+  const size_t pages = (c->M_max + kPage - 1) / kPage * kv_page_elems(c->s.Hkv, c->s.D);
+  *k = w.take<uint16_t>(pages);
+  *v = w.take<uint16_t>(pages);
+  *ws = w.take<char>(kvq_attention_workspace(c->s.Hq, c->s.Hkv, c->s.D, c->k_max + 1));
+  return (w.off + 255) & ~(size_t)255;
+}
+}  // namespace
+
+size_t bs_kvq_bind_bytes(const bs_ctx* c) {
+  if (!c || c->s.dtype != BS_BF16) return 0;
+  void *k, *v, *ws;
+  return kvq_bind_carve(c, nullptr, &k, &v, &ws);
+}
+bs_status bs_kvq_bind(bs_ctx* c, const bs_kvq_desc* layers, void* workspace, size_t workspace_bytes) {
+  if (!c) return BS_EINVAL;
+  if (!layers) { c->kvq.clear(); c->verify_pending = false; return BS_OK; }
+  if (c->s.dtype != BS_BF16) return fail(c, BS_EINVAL, "bs_kvq_bind: float32 models have no 8-bit cache");
+  if (!workspace || ((uintptr_t)workspace & 255)) return fail(c, BS_EINVAL, "bs_kvq_bind: workspace null or not on 256 bytes");
+  for (int l = 0; l < c->s.L; ++l) {
+    const bs_kvq_desc& d = layers[l];
+    const bs_status st = check_kvq(&d);
+    if (st != BS_OK) return fail(c, st, "bs_kvq_bind: bad description of a layer");
+    if (d.n_kv_heads != c->s.Hkv || d.head_dim != c->s.D || d.n_pages != c->kv.n_pages || d.n_slots != c->kv.n_slots || d.max_pages_per_seq != c->kv.max_pages)
+      return fail(c, BS_ESHAPE, "bs_kvq_bind: sizes differ from the context's");
+    if (d.block_table != c->kv.block_table) return fail(c, BS_EINVAL, "bs_kvq_bind: another block table than the context's");
+  }
+  if (!kvq_attention_counts(c->B_max, c->s.Hkv, c->s.Hq / c->s.Hkv, c->kv.max_pages, c->k_max + 1)) return fail(c, BS_ESHAPE, "bs_kvq_bind: too many tokens");
+  if (workspace_bytes < bs_kvq_bind_bytes(c)) return fail(c, BS_ECAPACITY, "bs_kvq_bind: workspace too small");
+  c->kvq.clear();
+  try {
+    c->kvq.reserve(c->s.L);
+  } catch (const std::bad_alloc&) {
+    return fail(c, BS_ECAPACITY, "bs_kvq_bind: out of host memory");
+  }
+  for (int l = 0; l < c->s.L; ++l) c->kvq.push_back(view_of(layers[l]));
+  kvq_bind_carve(c, (char*)workspace, &c->kvq_k, &c->kvq_v, &c->kvq_ws);
+  c->verify_pending = false;
+  return BS_OK;
 }
 
 size_t bs_token_logprobs_workspace_bytes(int B, int k_max, int vocab, int n_top) {

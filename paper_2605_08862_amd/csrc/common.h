@@ -230,10 +230,12 @@ struct KvView {
   int n_pages, n_slots, max_pages;
   const int32_t* block_table;
   int32_t* ctx_len;
+  bool staged = false;          // bs_kvq_bind: the step's rows go to staging pages in packed order, and from there to the 8-bit cache
 };
 
 // Cache place of a row, looked up once per step (block of a sequence -> slot -> page: three dependent loads that every append of every layer waited for).
 __device__ __forceinline__ void row_place(const Plan& p, const KvView& kv, int r) {
+  if (kv.staged) { p.row_kv[r] = r; return; }
   const int b = p.row_seq[r], pos = p.seq_c[b] + p.row_pos[r];
   p.row_kv[r] = kv.block_table[(size_t)p.seq_slot[b] * kv.max_pages + pos / kPage] * kPage + pos % kPage;
 }

@@ -73,8 +73,16 @@ __device__ __forceinline__ f32x4 kvq_values4(uint32_t c) {
 
 // kvq.hip   rows -> pages and back.  stride: elements from one row to the next.
 void launch_kvq_write(const KvqView& kv, const KvqSeqs& q, const void* k_rows, const void* v_rows, size_t stride, int32_t* status, hipStream_t st);
+// Rows that a verify step left in staging pages (16-bit page order): packed row r is token r % kPage of page r / kPage.
+void launch_kvq_write_staged(const KvqView& kv, const KvqSeqs& q, const void* k_pages, const void* v_pages, int32_t* status, hipStream_t st);
 void launch_kvq_read(const KvqView& kv, const KvqSeqs& q, void* k_rows, void* v_rows, size_t stride, int32_t* status, hipStream_t st);
 // kvq_attention.hip   q, out: [rows][Hq][D] bf16, q_stride elements from one row of q to the next
 size_t kvq_attention_workspace(int Hq, int Hkv, int D, int q_max);
 void launch_kvq_attention(const KvqView& kv, const KvqSeqs& q, int Hq, const void* qrows, size_t q_stride, void* out, int32_t* status, void* workspace,
                           hipStream_t st);
+// of a verify step: float16 queries [rows][Hq][D], output in chunk order (act_index, out_ld)
+void launch_kvq_step_attention(const KvqView& kv, const KvqSeqs& q, int Hq, const void* qrows, void* out, int out_ld, int32_t* status, void* workspace, hipStream_t st);
+// Whether steps of 128 tokens over all units, 38 for each at most, can be counted in 32 bits.
+inline bool kvq_attention_counts(int B, int Hkv, int G, int max_pages, int q_max) {
+  return (int64_t)B * Hkv * (max_pages / 2 + 1) <= ((int64_t)1 << 25) / ((int64_t)q_max * G / 128 + 1);
+}

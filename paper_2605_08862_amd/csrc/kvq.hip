@@ -322,6 +322,11 @@ void launch_kvq_write(const KvqView& kv, const KvqSeqs& q, const void* k_rows, c
   else { if (vec) BS_KVQ(ROWS_VEC, 64); else BS_KVQ(ROWS, 64); }
 #undef BS_KVQ
 }
+void launch_kvq_write_staged(const KvqView& kv, const KvqSeqs& q, const void* k_pages, const void* v_pages, int32_t* status, hipStream_t st) {
+  const dim3 grid(q.B * pages_each(q), kv.Hkv);
+  if (kv.D == 128) hipLaunchKernelGGL((kvq_write_kernel<STAGED, 128>), grid, dim3(256), 0, st, kv, q, pages_each(q), k_pages, v_pages, (size_t)0, status);
+  else hipLaunchKernelGGL((kvq_write_kernel<STAGED, 64>), grid, dim3(256), 0, st, kv, q, pages_each(q), k_pages, v_pages, (size_t)0, status);
+}
 void launch_kvq_read(const KvqView& kv, const KvqSeqs& q, void* k_rows, void* v_rows, size_t stride, int32_t* status, hipStream_t st) {
   const dim3 grid(q.B * pages_each(q), kv.Hkv);
   const bool vec = (((uintptr_t)k_rows | (uintptr_t)v_rows) & 15) == 0 && stride % 8 == 0;

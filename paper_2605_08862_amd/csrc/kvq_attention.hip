@@ -792,3 +792,8 @@ void launch_kvq_attention(const KvqView& kv, const KvqSeqs& s, int Hq, const voi
   if (kv.D == 128) launch<128, false>(kv, s, Hq, qrows, q_stride, o, status, workspace, st);
   else launch<64, false>(kv, s, Hq, qrows, q_stride, o, status, workspace, st);
 }
+void launch_kvq_step_attention(const KvqView& kv, const KvqSeqs& s, int Hq, const void* qrows, void* out, int out_ld, int32_t* status, void* workspace, hipStream_t st) {
+  const KvqOut o{out, out_ld};
+  if (kv.D == 128) launch<128, true>(kv, s, Hq, qrows, (size_t)Hq * kv.D, o, status, workspace, st);
+  else launch<64, true>(kv, s, Hq, qrows, (size_t)Hq * kv.D, o, status, workspace, st);
+}

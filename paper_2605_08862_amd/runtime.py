@@ -49,10 +49,10 @@ class Engine:
     """Owns the device buffers of one context and forwards to the C ABI."""
 
     def __init__(self, desc, weights, n_slots, max_ctx, B_max, k_max, device="cuda:0", page_perm_seed=None,
-                 slot_tokens=None):
+                 slot_tokens=None, kv_bits=16):
         """max_ctx: token capacity of every slot; slot_tokens (optional, one entry per slot) gives every slot its own
         capacity instead, so that a ragged batch only takes the pages it needs (block-table entries beyond a slot's
-        pages are -1)."""
+        pages are -1).  kv_bits = 8 (bf16 models): the cache holds 8 bits per element (KvqCache, bs_kvq_bind)."""
         self.desc = dict(desc)
         self.device = torch.device(device)
         self.cdesc = B.make_desc(desc)
@@ -65,11 +65,17 @@ class Engine:
         self.max_pages = self.block_table.shape[1]
         self.n_slots = n_slots
         page_elems = desc["n_kv_heads"] * P * desc["head_dim"]
-        # pages are zero-initialised: masked positions still enter the P*V product with weight 0
-        self.k_pages = [torch.zeros(self.n_pages, page_elems, dtype=td, device=self.device)
-                        for _ in range(desc["n_layers"])]
-        self.v_pages = [torch.zeros(self.n_pages, page_elems, dtype=td, device=self.device)
-                        for _ in range(desc["n_layers"])]
+        self.kvq = None
+        if kv_bits == 8:
+            self.kvq = KvqCache(desc["n_layers"], desc["n_q_heads"], desc["n_kv_heads"], desc["head_dim"], n_slots, max_ctx, k_max + 1,
+                                device=self.device, block_table=self.block_table, n_pages=self.n_pages)
+            self.k_pages, self.v_pages = self.kvq.k_pages, self.kvq.v_pages
+        else:
+            # pages are zero-initialised: masked positions still enter the P*V product with weight 0
+            self.k_pages = [torch.zeros(self.n_pages, page_elems, dtype=td, device=self.device)
+                            for _ in range(desc["n_layers"])]
+            self.v_pages = [torch.zeros(self.n_pages, page_elems, dtype=td, device=self.device)
+                            for _ in range(desc["n_layers"])]
         self.ctx_len = torch.zeros(n_slots, dtype=torch.int32, device=self.device)
         nbytes = B.bs_workspace_bytes(self.cdesc, B_max, k_max)
         if nbytes == 0:
@@ -78,6 +84,9 @@ class Engine:
         kv = dict(n_pages=self.n_pages, n_slots=n_slots, max_pages_per_seq=self.max_pages, k_pages=self.k_pages,
                   v_pages=self.v_pages, block_table=self.block_table, ctx_len=self.ctx_len)
         self.ctx = B.bs_create(self.cdesc, weights, kv, self.workspace, B_max, k_max)
+        if self.kvq is not None:
+            self._kvq_workspace = torch.zeros(max(B.bs_kvq_bind_bytes(self.ctx), 1), dtype=torch.uint8, device=self.device)
+            B.bs_kvq_bind(self.ctx, self.kvq.desc, self._kvq_workspace)
         self._pool = None
 
     def close(self):
@@ -179,10 +188,11 @@ class KvqCache:
     sequence, which are on the device.  `status` (one int32 on the device) collects BS_FAULT_* bits until poll_status."""
 
     def __init__(self, n_layers, n_q_heads, n_kv_heads, head_dim, n_slots, max_ctx, q_max, device="cuda:0", page_perm_seed=None,
-                 slot_tokens=None):
+                 slot_tokens=None, block_table=None, n_pages=0):
+        """block_table, n_pages: those of another owner (an Engine) instead of own ones."""
         self.device = torch.device(device)
         self.n_q_heads, self.n_kv_heads, self.head_dim, self.n_slots, self.q_max = n_q_heads, n_kv_heads, head_dim, n_slots, q_max
-        self.block_table, self.n_pages = page_table(n_slots, max_ctx, slot_tokens, page_perm_seed, self.device)
+        self.block_table, self.n_pages = (block_table, n_pages) if block_table is not None else page_table(n_slots, max_ctx, slot_tokens, page_perm_seed, self.device)
         page = n_kv_heads * B.BS_PAGE_TOKENS * head_dim
         zeros = lambda *shape, dtype: [torch.zeros(*shape, dtype=dtype, device=self.device) for _ in range(n_layers)]
         # zero-filled: masked positions still enter the P*V product with weight 0

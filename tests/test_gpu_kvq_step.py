@@ -1,0 +1,210 @@
+"""Verify steps over the 8-bit cache against the oracle decoder, and the operators run together as a rollout uses them.
+
+The rounding of a row to 8 bits turns a last-bit difference of a projection into a step of 2^-3 now and then, so the oracle attends to the
+rows that the device holds (read back through bs_kv_read), each of which is checked against the oracle's own row first; logits then have the
+tolerance of the 16-bit cache."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import decoder as OD
+from oracle import logprobs as OL
+from paper_2605_08862_amd import binding as B
+from paper_2605_08862_amd import workloads as W
+from paper_2605_08862_amd.runtime import Engine, LogprobScorer, fuse_weights
+from tests import helpers as H
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _f64_weights(wn):
+    c = lambda a: np.asarray(a, dtype=np.float64)
+    return {"embed": wn["embed"], "lm_head": c(wn["lm_head"]), "final_norm": c(wn["final_norm"]),
+            "layers": [{k: c(v) for k, v in lw.items()} for lw in wn["layers"]]}
+
+
+class HeldCache(OD.SeqCache):
+    """The oracle's cache of one slot, with the rows that the device holds."""
+
+    def __init__(self, desc, eng, slot):
+        super().__init__(desc)
+        self.eng, self.slot = eng, slot
+
+    def load(self, n):
+        if n == 0:
+            return
+        rows = [[t.double().cpu().numpy() for t in self.eng.kv_read(l, self.slot, 0, n)] for l in range(self.desc.n_layers)]
+        self.fill([k for k, _ in rows], [v for _, v in rows])
+
+    def append(self, layer, k_new, v_new):
+        c, n = self.committed, k_new.shape[0]
+        held = [t.double().cpu().numpy() for t in self.eng.kv_read(layer, self.slot, 0, c + n)]
+        scales = [float(s[layer].max()) for s in (self.eng.kvq.k_scale, self.eng.kvq.v_scale)]
+        for got, want, s in zip(held, (k_new, v_new), scales):
+            # half a step of e4m3 (2^-4 of the value, 2^-10 of the scale below 2^-6 of it) around what float16 operands leave of a projection
+            off = np.abs(got[c:] - want)
+            assert np.all(off <= 2.0 ** -4 * np.maximum(np.abs(got[c:]), np.abs(want)) + 2.0 ** -10 * s + 2e-2), off.max()
+        # older rows of the block that the new ones share may have been rounded again
+        self.k[layer], self.v[layer] = held
+
+
+def _engine(desc, seed, caps, k_max, B_max=None):
+    w = W.make_weights(desc, seed=seed)
+    eng = Engine(desc, fuse_weights(w, desc["dtype"], DEV), len(caps), max(caps), B_max=B_max or len(caps), k_max=k_max, page_perm_seed=3, slot_tokens=caps, kv_bits=8)
+    return eng, _f64_weights(W.weights_to_numpy(w))
+
+
+def _step(eng, wn, od, slots, ctx, k_b, k_max, rng, want_out=False):
+    """One verify step of the sequences in `slots` with committed lengths ctx, checked against the oracle.  Returns (drafts, logits rows)."""
+    n, V = len(slots), eng.desc["vocab"]
+    last, drafts = rng.integers(0, V, n), rng.integers(0, V, (n, k_max))
+    logits = eng.verify_step(H.dev_i32(slots), H.dev_i32(last), H.dev_i32(drafts), H.dev_i32(k_b), k_max, want_logits=True)
+    blocks = H.pack_rows(last, drafts, np.asarray(k_b))
+    ref = []
+    for b in range(n):
+        c = HeldCache(od, eng, slots[b])
+        c.load(ctx[b])
+        ref.append(OD.verify_block(od, wn, c, blocks[b]))
+    ref = np.concatenate(ref)
+    got = logits[:ref.shape[0]].cpu().numpy()
+    err = np.abs(got - ref).max()
+    assert err <= H.TOL_LOGITS[W.BS_BF16], err
+    assert eng.poll_status() == 0
+    return drafts, logits
+
+
+SHAPES = {
+    "d128_g3": W.shape("mini_bf16"),
+    "d128_g7": W.shape("mini_bf16", n_q_heads=7, n_kv_heads=1),
+    "d64": W.shape("mini_bf16", n_q_heads=4, n_kv_heads=4, head_dim=64),
+}
+
+
+@pytest.mark.parametrize("shape,ctx,k_b,k_max,unfused", [
+    ("d128_g3", [70, 0, 130], [4, 2, 0], 4, False),                        # a step of at most 32 rows
+    ("d128_g3", [70, 63, 130, 1, 200, 64], [8, 0, 5, 8, 7, 1], 8, False),  # more rows: fused QKV
+    ("d128_g3", [70, 63, 130, 1, 200, 64], [8, 0, 5, 8, 7, 1], 8, True),
+    ("d128_g7", [300, 40, 129, 0] * 9, [16, 3, 9, 14] * 9, 16, False),     # blocks of 128 rows
+    ("d64", [90, 0, 300], [3, 6, 6], 6, False),
+])
+def test_steps_match_the_oracle_on_the_held_rows(shape, ctx, k_b, k_max, unfused):
+    desc = SHAPES[shape]
+    rng = np.random.default_rng(len(ctx) * 10 + k_max)
+    n = len(ctx)
+    eng, wn = _engine(desc, 21, [c + 4 * (k_max + 1) for c in ctx], k_max)
+    if unfused:
+        B.bs_debug_unfused_qkv(eng.ctx, True)
+    od = H.oracle_desc(desc)
+    for b in range(n):
+        if ctx[b]:
+            for l, (k, v) in enumerate(W.context_kv(desc, ctx[b], 500 + b)):
+                eng.kv_write(l, b, 0, k.to(DEV), v.to(DEV))
+    eng.ctx_len.copy_(H.dev_i32(ctx))
+    slots = [int(s) for s in rng.permutation(n)]
+    for _ in range(2):                                                     # the second step writes over the rejected rows of the first
+        now = [int(c) for c in eng.kv_lengths(H.dev_i32(slots)).tolist()]
+        _step(eng, wn, od, slots, now, [k_b[s] for s in slots], k_max, rng)
+        keep = [int(rng.integers(0, k_b[s] + 2)) for s in slots]
+        eng.kv_commit(H.dev_i32(slots), H.dev_i32(keep))
+        assert eng.kv_lengths(H.dev_i32(slots)).tolist() == [c + k for c, k in zip(now, keep)]
+
+
+def test_a_rollout_step_with_everything_together():
+    """Verify over the 8-bit cache, accept, log probabilities of what was emitted (under the distribution that the step sampled from), commit;
+    eager, then captured into a graph and replayed with eager work in between: the same results each time."""
+    desc = SHAPES["d128_g3"]
+    k_max, n, V, T = 4, 5, desc["vocab"], 0.9
+    rng = np.random.default_rng(9)
+    ctx, k_b = [70, 5, 130, 64, 0], [4, 0, 3, 4, 1]
+    eng, _ = _engine(desc, 33, [c + 20 for c in ctx], k_max)
+    for b in range(n):
+        if ctx[b]:
+            for l, (k, v) in enumerate(W.context_kv(desc, ctx[b], 700 + b)):
+                eng.kv_write(l, b, 0, k.to(DEV), v.to(DEV))
+    slots, last, drafts, dl = H.dev_i32(np.arange(n)), H.dev_i32(rng.integers(0, V, n)), H.dev_i32(rng.integers(0, V, (n, k_max))), H.dev_i32(k_b)
+    ua, us = (H.dev_f32(u) for u in W.uniforms(5, n, k_max))
+    logits = torch.zeros(n * (k_max + 1), V, device=DEV)
+    scorer = LogprobScorer(n, k_max, V, 3, device=DEV)
+    out = {}
+
+    def step():
+        eng.ctx_len.copy_(ctx_dev)
+        B.bs_verify_step(eng.ctx, n, slots, last, drafts, dl, k_max, logits)
+        acc = eng.accept_resample(drafts, dl, k_max, ua, us, temperature=T)
+        lp = scorer(logits, acc["out_tokens"], acc["n_emitted"], dl, temperature=T)
+        n_commit = acc["n_accepted"] + 1
+        eng.kv_commit(slots, n_commit)
+        out.update(acc=acc, lp=lp)
+    ctx_dev = H.dev_i32(ctx)
+    step()
+    torch.cuda.synchronize()
+    first = {k: v.clone() for k, v in list(out["acc"].items()) + list(out["lp"].items())}
+    z, at = logits.cpu().numpy(), 0
+    emitted, toks = first["n_emitted"].tolist(), first["out_tokens"].tolist()
+    assert sum(emitted) >= n
+    for b in range(n):
+        for i in range(k_max + 1):
+            if i >= emitted[b]:
+                assert float(first["logprob"][b, i]) == 0.0
+                continue
+            lp, h, top, ltop = OL.row(z[at + i], toks[b][i], T, 3)
+            assert abs(float(first["logprob"][b, i]) - lp) < 1e-4 and abs(float(first["entropy"][b, i]) - h) < 1e-4
+            assert first["top_tokens"][b, i].tolist() == top.tolist() and np.allclose(first["top_logprobs"][b, i].cpu().numpy(), ltop, atol=1e-4)
+        at += k_b[b] + 1
+    lengths = eng.kv_lengths(slots).tolist()
+    g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    with torch.cuda.graph(g):
+        step()
+    for _ in range(3):
+        for t in list(out["acc"].values()) + list(out["lp"].values()):
+            t.fill_(-7)
+        g.replay()
+        torch.cuda.synchronize()
+        for k, v in list(out["acc"].items()) + list(out["lp"].items()):
+            assert torch.equal(v, first[k]), k
+        assert eng.kv_lengths(slots).tolist() == lengths and eng.poll_status() == 0 and scorer.poll_status() == 0
+        torch.randn(1000, device=DEV).sum().item()                         # the program's own work between replays
+
+
+def test_bind_and_unbind():
+    desc = SHAPES["d128_g3"]
+    eng, _ = _engine(desc, 1, [100, 100], 3)
+    ws, descs = eng._kvq_workspace, eng.kvq.desc
+    need = B.bs_kvq_bind_bytes(eng.ctx)
+
+    def refused(status, d=descs, w=ws):
+        with pytest.raises(B.BsError) as e:
+            B.bs_kvq_bind(eng.ctx, d, w)
+        assert e.value.status == status
+    refused(B.BS_ECAPACITY, w=ws[:need - 256])
+    refused(B.BS_EINVAL, w=ws[64:])
+    other = [B.bs_kvq_desc.from_buffer_copy(d) for d in descs]
+    other[1].n_kv_heads = 1
+    refused(B.BS_ESHAPE, d=other)
+    other = [B.bs_kvq_desc.from_buffer_copy(d) for d in descs]
+    other[0].block_table += 4
+    refused(B.BS_EINVAL, d=other)
+    other[0].block_table = 0
+    refused(B.BS_EINVAL, d=other)
+    # an engine with the 16-bit cache that has one bound and unbound works as if it never had
+    plain = Engine(desc, eng.weights, 2, 100, B_max=2, k_max=3)
+    args = (H.dev_i32([0, 1]), H.dev_i32([5, 6]), H.dev_i32([[1, 2, 3], [4, 5, 6]]), H.dev_i32([3, 1]), 3)
+    want = plain.verify_step(*args, want_logits=True)
+    d = [B.bs_kvq_desc.from_buffer_copy(x) for x in descs]
+    for x in d:
+        x.block_table = plain.block_table.data_ptr()
+    B.bs_kvq_bind(plain.ctx, d, ws)
+    with pytest.raises(B.BsError) as e:
+        plain.kv_commit(args[0], H.dev_i32([1, 1]))                        # the pending step is dropped
+    assert e.value.status == B.BS_ESTATE
+    B.bs_kvq_bind(plain.ctx, None, None)
+    assert torch.equal(plain.verify_step(*args, want_logits=True), want)
+    tiny = W.shape("tiny")
+    with pytest.raises(B.BsError) as e:
+        Engine(tiny, fuse_weights(W.make_weights(tiny, seed=1), tiny["dtype"], DEV), 1, 64, B_max=1, k_max=0, kv_bits=8)
+    assert e.value.status == B.BS_EINVAL
