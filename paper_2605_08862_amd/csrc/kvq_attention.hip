@@ -565,31 +565,91 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) kvq_attention_kernel(BS_
   });
 }
 
+// Queries as e4m3: q = 2^e (t0 + t1 / 16 + t2 / 256), every term an e4m3 value.  A term has four significant bits, so two hold a bf16 value and three a float16
+// value (what is lost is below 2^-22 of the row's largest element); e is the least with the row's largest element at most 448 * 2^e.  Scores from codes as they are
+// then need no conversion of K: 32 x 32 x 64 products, whose operands take scales 2^x of their own.
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ f32x16 mfma_codes(i32x8 a, i32x8 b, f32x16 c, int scale_a, int scale_b) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, scale_a, 0, scale_b);
+#else
+  return c;
+#endif
+}
+__device__ __forceinline__ int scale_byte(int e) { return min(max(e + 127, 1), 254); }
+// qf: the D / 16 float16 pieces of this lane (eight d each); t[term][MFMA]: sixteen bytes of two pieces each, in the order of K's codes.  Returns e.
+template <int D, int NT>
+__device__ __forceinline__ int split_query(const u32x4 (&qf)[D / 16], i32x8 (&t)[NT][D / 64]) {
+  float most = 0.f;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const f16x8 h = as_f16x8(qf[s]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf((float)h[j]));
+  }
+  most = max_halves(most);                              // the other half of the row's d
+  const uint32_t u = __float_as_uint(most);
+  const int e = max((int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), -60);
+  const float f = kvq_scale(-e);
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const f16x8 h = as_f16x8(qf[s]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = (float)h[4 * k + j] * f;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const uint32_t c = kvq_codes4(x[0], x[1], x[2], x[3]);
+        t[n][s / 4][(s % 4) * 2 + k] = (int)c;
+        const f32x4 y = kvq_values4(c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = (x[j] - y[j]) * 16.f;
+      }
+    }
+  }
+  return e;
+}
+
 // Waits until at most N of this wave's requests are in flight (and for its LDS accesses), then for the other waves.
 template <int N> __device__ __forceinline__ void wait_requests() {
 #if defined(__HIP_DEVICE_COMPILE__)
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 #endif
 }
-// A wave's sixteen bytes per lane from memory to 1 KiB of LDS (dst: the same in all lanes).
+// A word or sixteen bytes of each lane from memory to LDS (dst: the same in all lanes, the first lane's place).
+__device__ __forceinline__ void copy_word_to_lds(const void* src, char* dst) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
+#endif
+}
 __device__ __forceinline__ void copy_to_lds(const uint8_t* src, char* dst) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 #endif
 }
 
-// Blocks of up to 128 rows, eight waves: wave w has query tile w % NQT and token phase w / NQT, NQT = 2 or 4 tiles by the rows of the unit; the 8 / NQT phases
-// work on different token tiles.  The waves of a phase share a tile of codes in LDS: the memory pipeline copies it there (global -> LDS loads, a share of the
-// 1 KiB pieces by each wave), NB buffers for each phase, NB - 1 tiles in flight and one barrier per tile; each wave converts what it multiplies.
+// Blocks of up to 128 rows, eight waves: NQT = 2 or 4 query tiles by the rows of the unit and NPH = 8 / NQT token phases, which work on different token tiles; wave
+// w has phase w % NPH of query tile w / NPH, so that the waves of a SIMD (w % 4) are of different query tiles.  The waves of a phase share a tile of codes in LDS:
+// the memory pipeline copies it there (global -> LDS loads, a share of the 1 KiB pieces by each wave), NB buffers for each phase, NB - 1 tiles in flight and one
+// barrier per tile.
+// What bounds it: two query tiles, memory; four, the vector instructions of softmax and the conversion of V, and what the two waves of a SIMD wait for each other
+// (of the 2250 cycles of an iteration a wave spent 1250 .. 1640 on its tile, 310 .. 430 on its requests when it asked for the page id there, 90 .. 660 waiting).  7B heads,
+// 32 sequences of 8192 tokens, 9 rows 68 us, 17 rows 96.  Two tiles per barrier: 101; twelve waves with three phases: 79 and 105; scores of the next tile
+// multiplied while this one's become probabilities: 10 us more.
 template <int D> constexpr int kWideStage = 96 * 1024 * D / 128;
+constexpr int kWideScales = 6 * 8 * 256;                // [buffers][waves] K and V scale in the first two words
 template <int D, bool STEP>
 __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
-  constexpr int KS = D / 16, DT = D / 32, RP = 128, CH = D / 4, NF = 2 * DT;     // NF: 1 KiB pieces of a tile, K then V
+  constexpr int KS = D / 16, DT = D / 32, RP = 128, CH = D / 4;
   constexpr int DH = D / 2, LDO = DH + 4;               // the accumulators are merged in two halves of the columns
+  constexpr int NT = STEP ? 3 : 2;                      // e4m3 terms of a query: float16 or bf16
   extern __shared__ __align__(16) char lds_raw[];
   __shared__ int s_scan[16], s_bad, s_flag;
-  float* const s_o = (float*)lds_raw;                   // [8][32][LDO], on top of the tiles
-  float* const s_m = (float*)(lds_raw + kWideStage<D>); // [8][32]
+  float* const s_o = (float*)lds_raw;                   // [8][32][LDO], on top of the codes
+  char* const s_scale = lds_raw + kWideStage<D>;
+  float* const s_m = (float*)(s_scale + kWideScales);   // [8][32]
   float* const s_l = s_m + 8 * 32;
   int* const s_start = (int*)(s_l + 8 * 32);            // [B + 1]
   int* const s_row = s_start + B + 1;                   // [B + 1]
@@ -599,30 +659,28 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
   const Shares sh = find_shares<512, true>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, least, s_start, s_row, s_scan, status);
 
   auto run = [&](auto nqt_tag, const Part& un) {
-    constexpr int NQT = decltype(nqt_tag)::value, NPH = 8 / NQT, LPW = NF / NQT;
+    constexpr int NQT = decltype(nqt_tag)::value, NPH = 8 / NQT;
+    constexpr int NF = 2 * DT, LPW = NF / NQT;          // 1 KiB pieces of a tile, K then V; of those a wave moves
     constexpr int NB = kWideStage<D> / (NPH * NF * 1024);     // buffers: 3 or 6
     const int32_t* __restrict__ bt = block_table + (size_t)seq_slot[un.b] * max_pages;
-    const int qt = wave % NQT, ph = wave / NQT;
+    const int qt = wave / NPH, ph = wave % NPH;
     const bool has_rows = qt * 32 < un.R;               // a wave without query rows only moves data
-    const int t_begin = 4 * un.s_lo, t_end = min(4 * un.s_hi, un.n_tiles);
-    const int n_it = (t_end - t_begin + NPH - 1) / NPH;
+    const int t_begin = 4 * un.s_lo, t_end = min(4 * un.s_hi, un.n_tiles), n_it = (t_end - t_begin + NPH - 1) / NPH;
     bool bad = false;
     auto tile_of = [&](int i) { return min(t_begin + ph + NPH * i, un.n_tiles - 1); };   // a phase without a tile moves the last one again
-    auto page_of = [&](int t) {
-      const int page = bt[t * kTile / kPage];
-      if ((unsigned)page < (unsigned)n_pages) return page;
-      bad = true;
-      return 0;
-    };
-    const size_t head = (size_t)un.h * 2 * (kTile * D) + lane * 16;
-    auto request = [&](int t, int buf) {                // this wave's share of a tile: pieces qt, qt + NQT, ..
-      const size_t off = (size_t)page_of(t) * ((size_t)Hkv * kPage * D) + (size_t)(t & 1) * (kTile * D) + head;
+    auto page_of = [&](int i) { return bt[tile_of(i) * kTile / kPage]; };
+    const size_t head = (size_t)un.h * (kPage * D) + lane * 16;
+    auto request = [&](int page, int i, int buf) {      // this wave's share: pieces qt, qt + NQT, ..
+      if ((unsigned)page >= (unsigned)n_pages) { bad = true; page = 0; }
+      const size_t off = (size_t)page * ((size_t)Hkv * kPage * D) + (size_t)(tile_of(i) & 1) * (kTile * D) + head;
 #pragma unroll
       for (int j = 0; j < LPW; ++j) {
         const int f = qt + NQT * j;
         const bool is_k = NQT * (j + 1) <= DT ? true : NQT * j >= DT ? false : f < DT;
         copy_to_lds((is_k ? k_pages : v_pages) + off + (is_k ? f : f - DT) * 1024, lds_raw + ((size_t)(buf * NPH + ph) * NF + f) * 1024);
       }
+      // the scales the same way: as scalar loads they were a trip to memory that every iteration waited for
+      copy_word_to_lds((lane == 0 ? k_scale : v_scale) + (size_t)page * Hkv + un.h, s_scale + (buf * 8 + wave) * 256);
     };
     const int qr = qt * 32 + ln;
     const int lim = qr < un.R ? un.c + G.div(un.qr0 + qr) : -1;
@@ -634,45 +692,57 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
       for (int s = 0; s < KS; ++s) qf[s] = *(const u32x4*)(src + s * 8);
     }
     // the query loads in front and the requests unconditional, so that the wait for the queries leaves the requests in flight
+    int first_pages[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) first_pages[i] = page_of(i);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < NB - 1; ++i) request(tile_of(i), i);
+    for (int i = 0; i < NB - 1; ++i) request(first_pages[i], i, i);
+    int next_page = first_pages[NB - 1];
     __builtin_amdgcn_sched_barrier(0);
     bool range = false;
 #pragma unroll
     for (int s = 0; s < KS; ++s) { asm volatile("" : "+v"(qf[s])); qf[s] = query8<STEP>(qf[s], range); }
+    i32x8 qt8[NT][D / 64];
+    const int q_exp = split_query<D, NT>(qf, qt8);
     f32x16 o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
-    int page = page_of(tile_of(0)), buf = 0;
-    float ks = k_scale[(size_t)page * Hkv + un.h], vs = v_scale[(size_t)page * Hkv + un.h];
+    int buf = 0;
     for (int i = 0; i < n_it; ++i) {
       // this wave's share of tile i has arrived (the up to NB - 2 requested behind it may be in flight), then everybody's; nobody reads tile i - 1 any more,
-      // whose buffer takes tile i + NB - 1.  The last tiles have NB - 1 requests of tiles behind the end in their place: the counts hold all the way.
-      wait_requests<(NB - 2) * LPW>();
+      // whose buffer takes tile i + NB - 1.  Behind the end the last one is requested again: the counts hold all the way.
+      wait_requests<(NB - 2) * (LPW + 1)>();
       __builtin_amdgcn_sched_barrier(0);
-      request(tile_of(i + NB - 1), buf == 0 ? NB - 1 : buf - 1);
+      request(next_page, i + NB - 1, buf == 0 ? NB - 1 : buf - 1);
+      next_page = page_of(i + NB);
       __builtin_amdgcn_sched_barrier(0);
       const int t = t_begin + ph + NPH * i;
-      page = page_of(tile_of(i + 1));
-      const float ks1 = k_scale[(size_t)page * Hkv + un.h], vs1 = v_scale[(size_t)page * Hkv + un.h];
       if (has_rows && t < t_end) {
-        const char* stage = lds_raw + (size_t)(buf * NPH + ph) * NF * 1024 + lane * 16;
+        const char* at = lds_raw + (size_t)(buf * NPH + ph) * NF * 1024 + lane * 16;
+        const u32x2 scales = *(const u32x2*)(s_scale + (buf * 8 + wave) * 256);
+        const int ks = (int)(scales[0] >> 23 & 255);    // exponents of powers of two are scale bytes
+        const float vs = __uint_as_float(scales[1]);
         u32x4 kc[DT], vc[DT];
 #pragma unroll
-        for (int s = 0; s < DT; ++s) kc[s] = *(const u32x4*)(stage + s * 1024);
+        for (int s = 0; s < DT; ++s) kc[s] = *(const u32x4*)(at + s * 1024);
         __builtin_amdgcn_sched_barrier(0);
         f32x16 st;
 #pragma unroll
         for (int r = 0; r < 16; ++r) st[r] = 0.f;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) st = mfma32(values8(kc[s / 2][2 * (s % 2)], kc[s / 2][2 * (s % 2) + 1], ks), as_f16x8(qf[s]), st);
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+          for (int x = 0; x < D / 64; ++x) {
+            const i32x8 ka{(int)kc[2 * x][0], (int)kc[2 * x][1], (int)kc[2 * x][2], (int)kc[2 * x][3], (int)kc[2 * x + 1][0], (int)kc[2 * x + 1][1], (int)kc[2 * x + 1][2], (int)kc[2 * x + 1][3]};
+            st = mfma_codes(ka, qt8[u][x], st, ks, scale_byte(q_exp - 4 * u));
+          }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int s = 0; s < DT; ++s) vc[s] = *(const u32x4*)(stage + (DT + s) * 1024);
+        for (int s = 0; s < DT; ++s) vc[s] = *(const u32x4*)(at + (DT + s) * 1024);
         __builtin_amdgcn_sched_barrier(0);
         f16x8 pf[2];
         softmax_tile<DT>(st, (t + 1) * kTile - 1 <= un.c_all, t * kTile + 16 * lg, lim, scale_log2e, m_run, l_run, o, pf);
@@ -681,13 +751,11 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
 #pragma unroll
           for (int t2 = 0; t2 < 2; ++t2) o[dt] = mfma32(values8(vc[dt][2 * t2], vc[dt][2 * t2 + 1], vs), pf[t2], o[dt]);
       }
-      ks = ks1;
-      vs = vs1;
       buf = buf == NB - 1 ? 0 : buf + 1;
     }
     if (bad && lane == 0) s_bad = 1;
     if (range && status) atomicOr(status, BS_FAULT_RANGE);
-    wait_requests<0>();                                 // the tiles' buffers become the accumulators'
+    wait_requests<0>();                                 // the codes' buffers become the accumulators'
 
     // ---- merge of the phases of every query tile, half of the columns at a time
     const uint32_t part = partial_row<RP>(w_id, w_id == un.w_first);
@@ -712,14 +780,14 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
         const int r = it / (CH / 2), ch = it % (CH / 2), tq = r / 32, lr = r % 32;
         float mw[NPH], mt = -INFINITY, lt = 0.f;
 #pragma unroll
-        for (int w = 0; w < NPH; ++w) { mw[w] = s_m[(w * NQT + tq) * 32 + lr]; mt = fmaxf(mt, mw[w]); }
+        for (int w = 0; w < NPH; ++w) { mw[w] = s_m[(tq * NPH + w) * 32 + lr]; mt = fmaxf(mt, mw[w]); }
         f32x4 acc{0.f, 0.f, 0.f, 0.f};
         if (mt != -INFINITY)
 #pragma unroll
           for (int w = 0; w < NPH; ++w) {
             const float f = __builtin_amdgcn_exp2f(mw[w] - mt);
-            lt += s_l[(w * NQT + tq) * 32 + lr] * f;
-            const f32x4 v = *(const f32x4*)(s_o + ((size_t)(w * NQT + tq) * 32 + lr) * LDO + ch * 4);
+            lt += s_l[(tq * NPH + w) * 32 + lr] * f;
+            const f32x4 v = *(const f32x4*)(s_o + ((size_t)(tq * NPH + w) * 32 + lr) * LDO + ch * 4);
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] += v[e] * f;
           }
@@ -771,7 +839,7 @@ void launch(const KvqView& kv, const KvqSeqs& s, int Hq, const void* q, size_t q
   float* ml = (float*)(counters + kLevels * kMaxShares);
   const Parts parts{ml + (size_t)kLevels * 2 * kMaxShares * RP * 2, ml, counters};
   const size_t lists = (size_t)(s.B + 1) * 8;
-  const size_t lds = wide ? kWideStage<D> + 2 * 8 * 32 * 4 + lists : (size_t)4 * 32 * (D + 4) * 4 + 2 * 4 * 32 * 4 + lists;
+  const size_t lds = wide ? kWideStage<D> + kWideScales + 2 * 8 * 32 * 4 + lists : (size_t)4 * 32 * (D + 4) * 4 + 2 * 4 * 32 * 4 + lists;
   auto kern = wide ? kvq_wide_kernel<D, STEP> : kvq_attention_kernel<1, D, STEP>;
   static const hipError_t set[2] = {hipFuncSetAttribute((const void*)kvq_wide_kernel<D, STEP>, hipFuncAttributeMaxDynamicSharedMemorySize, 144 * 1024),
                                     hipFuncSetAttribute((const void*)kvq_attention_kernel<1, D, STEP>, hipFuncAttributeMaxDynamicSharedMemorySize, 112 * 1024)};
