@@ -310,7 +310,7 @@ bs_status bs_kvq_read(const bs_kvq_desc* kv, int B, const int32_t* seq_slot, con
  * smaller) is zero-filled once before its first use; calls that share one must not overlap in time.
  * Errors: BS_EINVAL (null, q or out not on 16 bytes, q_stride not a multiple of 8, misaligned workspace), BS_ESHAPE (as above;
  * n_q_heads not a multiple of n_kv_heads or more than 128 to one, q_max outside [1, max_pages_per_seq * BS_PAGE_TOKENS],
- * B * n_kv_heads * (max_pages_per_seq / 2 + 1) * (q_max * n_q_heads / n_kv_heads / 128 + 1) above 2^25), BS_ECAPACITY (workspace too small), BS_EHIP. */
+ * B * n_kv_heads * (max_pages_per_seq / 2 + 1) * (q_max * n_q_heads / n_kv_heads / 128 + 1) above 2^24), BS_ECAPACITY (workspace too small), BS_EHIP. */
 size_t bs_kvq_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim, int q_max);   /* 0 on invalid arguments */
 bs_status bs_kvq_attention(const bs_kvq_desc* kv, int B, const int32_t* seq_slot /*[B]*/, const int32_t* ctx_len /*[B]*/,
                            const int32_t* q_len /*[B]*/, int q_max, int n_q_heads, const void* q, int64_t q_stride, void* out,

@@ -37,11 +37,12 @@ __device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
 }
 
 // ---- the shares ------------------------------------------------------------------------------------------------------------------
-// All units in a row (sequence, KV head, block) have a length: kUnitCost and step_cost for each of their steps, in units of 1/8 step of a launch that is bound
+// All units in a row (sequence, KV head, block) have a length: kUnitHalf, step_cost for each of their steps, kUnitHalf, in units of 1/8 step of a launch that is bound
 // by memory.  The workgroups cut that into W equal parts; a cut is moved to the next step's start, and to the unit's end or start where less than kSnap + 1
 // steps would be left on that side.  So a share is a run of steps, and what a unit costs besides its steps (its queries, the merge of the waves) counts.
-constexpr int kUnitCost = 24, kSnap = 2;
-template <bool WIDE> __device__ __forceinline__ int step_cost(int R) { return WIDE && R > 64 ? 14 : 8; }
+constexpr int kSnap = 2;
+template <bool WIDE> constexpr int kUnitHalf = WIDE ? 40 : 8;             // on either side of a unit's steps
+template <bool WIDE> __device__ __forceinline__ int step_cost(int R) { return WIDE && R > 64 ? 12 : 8; }
 template <bool WIDE> constexpr int kBlock = WIDE ? 128 : 32;          // rows of a block
 // Query heads of a KV head.  x / g by a product with 2^32 / g rounded up: exact for x below 2^32 / g, i.e. any packed row.
 struct Group {
@@ -89,7 +90,7 @@ __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_sl
     if (slot < 0 || slot >= n_slots) { fault |= BS_FAULT_SLOT; continue; }
     if (c < 0 || (long long)c + n > (long long)max_pages * kPage) { fault |= BS_FAULT_KV_PAGES; continue; }
     int s = 0;
-    for (int qb = sub; qb * RP < n * G.g; qb += subs) s += kUnitCost + step_cost<WIDE>(n * G.g - qb * RP) * block_steps<RP>(c, n, G, qb);
+    for (int qb = sub; qb * RP < n * G.g; qb += subs) s += 2 * kUnitHalf<WIDE> + step_cost<WIDE>(n * G.g - qb * RP) * block_steps<RP>(c, n, G, qb);
     cost += s * Hkv;
   }
   for (int o = 1; o < subs; o <<= 1) cost += __shfl_xor(cost, o);
@@ -121,28 +122,29 @@ __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_sl
   return sh;
 }
 
+template <bool WIDE>
 struct Unit {
   int b, h, qb, blocks;                                 // sequence, KV head, block of its blocks
   int n, c, row0;                                       // rows of the sequence, tokens before them, first packed row
   int first, steps, step;                               // where the unit begins, its steps, what one costs
-  __device__ __forceinline__ int end() const { return first + kUnitCost + step * steps; }
+  __device__ __forceinline__ int end() const { return first + 2 * kUnitHalf<WIDE> + step * steps; }
   // step at which a cut at p is made
   __device__ __forceinline__ int cut(int p) const {
-    const int x = max(p - first - kUnitCost, 0) + step - 1, j = step == 8 ? x >> 3 : (int)__umulhi((uint32_t)x, 306783379u);   // / step, 8 or 14
-    return p >= end() ? steps : p <= first + kUnitCost + kSnap * step ? 0 : steps - j <= kSnap ? steps : j;
+    const int x = max(p - first - kUnitHalf<WIDE>, 0) + step - 1, j = step == 8 ? x >> 3 : (int)__umulhi((uint32_t)x, 357913942u);   // / step, 8 or 12
+    return p >= end() ? steps : p <= first + kUnitHalf<WIDE> + kSnap * step ? 0 : steps - j <= kSnap ? steps : j;
   }
   // the first and the last workgroup that have steps of the unit
-  __device__ __forceinline__ int first_share(const Shares& sh) const { return sh.of(min(first + kUnitCost + kSnap * step, sh.total - 1)); }
-  __device__ __forceinline__ int last_share(const Shares& sh) const { return sh.of(first + kUnitCost + max(step * (steps - kSnap - 1), kSnap * step)); }
+  __device__ __forceinline__ int first_share(const Shares& sh) const { return sh.of(min(first + kUnitHalf<WIDE> + kSnap * step, sh.total - 1)); }
+  __device__ __forceinline__ int last_share(const Shares& sh) const { return sh.of(first + kUnitHalf<WIDE> + max(step * (steps - kSnap - 1), kSnap * step)); }
 };
 template <bool WIDE>
-__device__ __forceinline__ void fill_unit(Unit& u, Group G) {
+__device__ __forceinline__ void fill_unit(Unit<WIDE>& u, Group G) {
   constexpr int RP = kBlock<WIDE>;
   u.steps = block_steps<RP>(u.c, u.n, G, u.qb);
   u.step = step_cost<WIDE>(u.n * G.g - u.qb * RP);
 }
 template <bool WIDE>
-__device__ __forceinline__ void enter_sequence(Unit& u, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add, Group G) {
+__device__ __forceinline__ void enter_sequence(Unit<WIDE>& u, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add, Group G) {
   u.b = __builtin_amdgcn_readfirstlane(u.b);
   u.n = seq_n[u.b] + n_add;
   u.c = seq_pos[u.b];
@@ -154,9 +156,9 @@ __device__ __forceinline__ void enter_sequence(Unit& u, const int* s_start, cons
 }
 // The unit that p (below the total) lies in.
 template <bool WIDE>
-__device__ __forceinline__ Unit unit_at(int p, int B, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
+__device__ __forceinline__ Unit<WIDE> unit_at(int p, int B, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
                                         Group G, int Hkv) {
-  Unit u;
+  Unit<WIDE> u;
   int lo = 0, hi = B;                                   // largest b with s_start[b] <= p (sequences without units are passed over)
   while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_start[mid] <= p) lo = mid; else hi = mid; }
   u.b = lo;
@@ -172,7 +174,7 @@ __device__ __forceinline__ Unit unit_at(int p, int B, const int* s_start, const 
 }
 // The unit behind; false behind the last one.
 template <bool WIDE>
-__device__ __forceinline__ bool next_unit(Unit& u, int B, int Hkv, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n,
+__device__ __forceinline__ bool next_unit(Unit<WIDE>& u, int B, int Hkv, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n,
                                           int n_add, Group G) {
   u.first = u.end();
   if (++u.qb < u.blocks) { fill_unit<WIDE>(u, G); return true; }
@@ -189,7 +191,7 @@ struct Part {
   bool whole;
 };
 template <bool WIDE>
-__device__ __forceinline__ Part part_of(const Unit& u, const Shares& sh, int s_lo, int s_hi, Group G) {
+__device__ __forceinline__ Part part_of(const Unit<WIDE>& u, const Shares& sh, int s_lo, int s_hi, Group G) {
   constexpr int RP = kBlock<WIDE>;
   Part t;
   t.b = u.b; t.h = u.h; t.row0 = u.row0; t.c = u.c;
@@ -213,7 +215,7 @@ __device__ __forceinline__ void for_parts(const Shares& sh, int B, const int* s_
   const int w = blockIdx.x;
   if (w >= sh.W || sh.total == 0) return;
   const int p0 = __builtin_amdgcn_readfirstlane(sh.bound(w)), p1 = __builtin_amdgcn_readfirstlane(sh.bound(w + 1));
-  Unit u = unit_at<WIDE>(p0, B, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv);
+  Unit<WIDE> u = unit_at<WIDE>(p0, B, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv);
   int s_lo = u.cut(p0);
   while (true) {
     const bool last = u.end() >= p1;
@@ -832,7 +834,7 @@ void launch(const KvqView& kv, const KvqSeqs& s, int Hq, const void* q, size_t q
   const bool wide = runs_wide(s, Hq / kv.Hkv, kv.Hkv);
   const int RP = wide ? 128 : 32, G = Hq / kv.Hkv, least = 32;
   // no more workgroups than shares, of sequences as long as the block table is wide
-  const long long blocks = ((long long)s.n_max * G + RP - 1) / RP, most = (long long)s.B * kv.Hkv * blocks * (kUnitCost + 14 * (kv.max_pages / 2 + 1)) / least + 1;
+  const long long blocks = ((long long)s.n_max * G + RP - 1) / RP, most = (long long)s.B * kv.Hkv * blocks * (2 * (wide ? kUnitHalf<true> : kUnitHalf<false>) + 12 * (kv.max_pages / 2 + 1)) / least + 1;
   const int grid = (int)(most < workgroups(wide) ? most : workgroups(wide));
   const uint32_t g_recip = G == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + G - 1) / G);
   int32_t* counters = (int32_t*)workspace;
