@@ -125,7 +125,7 @@ __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_sl
 template <bool WIDE>
 struct Unit {
   int b, h, qb, blocks;                                 // sequence, KV head, block of its blocks
-  int n, c, row0;                                       // rows of the sequence, tokens before them, first packed row
+  int n, c, row0, slot;                                 // rows of the sequence, tokens before them, first packed row
   int first, steps, step;                               // where the unit begins, its steps, what one costs
   __device__ __forceinline__ int end() const { return first + 2 * kUnitHalf<WIDE> + step * steps; }
   // step at which a cut at p is made
@@ -144,10 +144,11 @@ __device__ __forceinline__ void fill_unit(Unit<WIDE>& u, Group G) {
   u.step = step_cost<WIDE>(u.n * G.g - u.qb * RP);
 }
 template <bool WIDE>
-__device__ __forceinline__ void enter_sequence(Unit<WIDE>& u, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add, Group G) {
+__device__ __forceinline__ void enter_sequence(Unit<WIDE>& u, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add, Group G) {
   u.b = __builtin_amdgcn_readfirstlane(u.b);
   u.n = seq_n[u.b] + n_add;
   u.c = seq_pos[u.b];
+  u.slot = seq_slot[u.b];
   u.row0 = __builtin_amdgcn_readfirstlane(s_row[u.b]);
   u.first = __builtin_amdgcn_readfirstlane(s_start[u.b]);
   u.blocks = (u.n * G.g + kBlock<WIDE> - 1) / kBlock<WIDE>;
@@ -156,13 +157,13 @@ __device__ __forceinline__ void enter_sequence(Unit<WIDE>& u, const int* s_start
 }
 // The unit that p (below the total) lies in.
 template <bool WIDE>
-__device__ __forceinline__ Unit<WIDE> unit_at(int p, int B, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
+__device__ __forceinline__ Unit<WIDE> unit_at(int p, int B, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
                                         Group G, int Hkv) {
   Unit<WIDE> u;
   int lo = 0, hi = B;                                   // largest b with s_start[b] <= p (sequences without units are passed over)
   while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_start[mid] <= p) lo = mid; else hi = mid; }
   u.b = lo;
-  enter_sequence<WIDE>(u, s_start, s_row, seq_pos, seq_n, n_add, G);
+  enter_sequence<WIDE>(u, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G);
   const int all = __builtin_amdgcn_readfirstlane(s_start[u.b + 1]) - u.first, head = u.blocks == 1 ? u.end() - u.first : all / Hkv;
   int h = min(Hkv - 1, (int)((float)(p - u.first) / (float)head));
   while (h > 0 && h * head > p - u.first) --h;
@@ -174,19 +175,19 @@ __device__ __forceinline__ Unit<WIDE> unit_at(int p, int B, const int* s_start, 
 }
 // The unit behind; false behind the last one.
 template <bool WIDE>
-__device__ __forceinline__ bool next_unit(Unit<WIDE>& u, int B, int Hkv, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n,
-                                          int n_add, Group G) {
+__device__ __forceinline__ bool next_unit(Unit<WIDE>& u, int B, int Hkv, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos,
+                                          const int32_t* __restrict__ seq_n, int n_add, Group G) {
   u.first = u.end();
   if (++u.qb < u.blocks) { fill_unit<WIDE>(u, G); return true; }
   u.qb = 0;
   if (++u.h < Hkv) { fill_unit<WIDE>(u, G); return true; }
   do { if (++u.b >= B) return false; } while (s_start[u.b + 1] == s_start[u.b]);
-  enter_sequence<WIDE>(u, s_start, s_row, seq_pos, seq_n, n_add, G);
+  enter_sequence<WIDE>(u, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G);
   return true;
 }
 // What a workgroup does of a unit.
 struct Part {
-  int b, h, row0, qr0, R, c, s_lo, s_hi, n_tiles, c_all;   // qr0: first row (query row x head) of the block in the sequence; c_all: last position that every row sees
+  int slot, h, row0, qr0, R, c, s_lo, s_hi, n_tiles, c_all;   // qr0: first row (query row x head) of the block in the sequence; c_all: last position that every row sees
   int w_first, w_last;                                     // workgroups that have a part
   bool whole;
 };
@@ -194,7 +195,7 @@ template <bool WIDE>
 __device__ __forceinline__ Part part_of(const Unit<WIDE>& u, const Shares& sh, int s_lo, int s_hi, Group G) {
   constexpr int RP = kBlock<WIDE>;
   Part t;
-  t.b = u.b; t.h = u.h; t.row0 = u.row0; t.c = u.c;
+  t.slot = u.slot; t.h = u.h; t.row0 = u.row0; t.c = u.c;
   t.qr0 = u.qb * RP;
   t.R = min(u.n * G.g - t.qr0, RP);
   t.s_lo = s_lo; t.s_hi = s_hi;
@@ -210,19 +211,22 @@ __device__ __forceinline__ Part part_of(const Unit<WIDE>& u, const Shares& sh, i
 }
 // Calls f(part) for every part of this workgroup's share.
 template <bool WIDE, typename F>
-__device__ __forceinline__ void for_parts(const Shares& sh, int B, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n,
-                                          int n_add, Group G, int Hkv, const F& f) {
+__device__ __forceinline__ void for_parts(const Shares& sh, int B, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos,
+                                          const int32_t* __restrict__ seq_n, int n_add, Group G, int Hkv, const F& f) {
   const int w = blockIdx.x;
   if (w >= sh.W || sh.total == 0) return;
   const int p0 = __builtin_amdgcn_readfirstlane(sh.bound(w)), p1 = __builtin_amdgcn_readfirstlane(sh.bound(w + 1));
-  Unit<WIDE> u = unit_at<WIDE>(p0, B, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv);
+  Unit<WIDE> u = unit_at<WIDE>(p0, B, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G, Hkv);
   int s_lo = u.cut(p0);
   while (true) {
     const bool last = u.end() >= p1;
     const int s_hi = last ? u.cut(p1) : u.steps;
-    if (s_lo < s_hi) f(part_of<WIDE>(u, sh, s_lo, s_hi, G));
+    const Unit<WIDE> now = u;
+    // the next unit is looked up in front of this one's work, which covers the trip to memory
+    const bool more = !last && next_unit<WIDE>(u, B, Hkv, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G);
+    if (s_lo < s_hi) f(part_of<WIDE>(now, sh, s_lo, s_hi, G));
     s_lo = 0;
-    if (last || !next_unit<WIDE>(u, B, Hkv, s_start, s_row, seq_pos, seq_n, n_add, G)) break;
+    if (!more) break;
   }
 }
 // Partial rows: two places for each workgroup, for a unit that began before its share and for one that goes on behind it.
@@ -328,7 +332,8 @@ __device__ __forceinline__ void merge_unit(const Part& un, const Parts& p, const
     const bool last = stride * F >= n;
     if (count > 1) {
       if (!publish_arrival(p.counters + level * kMaxShares + un.w_first + i, count, s_flag)) return;
-      if (few) merge_group<THREADS, RP, D, STEP, 1, 8>(un, p, level, i, stride, count, last, out, Hq, G, status);
+      if (count == 2 && !few) merge_group<THREADS, RP, D, STEP, 8, 2>(un, p, level, i, stride, count, last, out, Hq, G, status);
+      else if (few) merge_group<THREADS, RP, D, STEP, 1, 8>(un, p, level, i, stride, count, last, out, Hq, G, status);
       else merge_group<THREADS, RP, D, STEP, 4, 4>(un, p, level, i, stride, count, last, out, Hq, G, status);
     } else {                                            // nothing to merge with on this level
       const wt_buf bm = wt_buffer(p.ml);
@@ -418,8 +423,8 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) kvq_attention_kernel(BS_
   const Group G{g_n, g_recip};
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, ln = lane & 31, lg = lane >> 5;
   const Shares sh = find_shares<256, false>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, least, s_start, s_row, s_scan, status);
-  for_parts<false>(sh, B, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv, [&](const Part& un) {
-    const int32_t* __restrict__ bt = block_table + (size_t)seq_slot[un.b] * max_pages;
+  for_parts<false>(sh, B, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G, Hkv, [&](const Part& un) {
+    const int32_t* __restrict__ bt = block_table + (size_t)un.slot * max_pages;
     const int t0 = 4 * un.s_lo + wave, t_end = min(4 * un.s_hi, un.n_tiles);
     const int n_my = t0 < t_end ? (t_end - t0 + 3) / 4 : 0, t_last = t0 + (n_my - 1) * 4;
     bool bad = false;
@@ -579,28 +584,53 @@ __device__ __forceinline__ f32x16 mfma_codes(i32x8 a, i32x8 b, f32x16 c, int sca
 #endif
 }
 __device__ __forceinline__ int scale_byte(int e) { return min(max(e + 127, 1), 254); }
-// qf: the D / 16 float16 pieces of this lane (eight d each); t[term][MFMA]: sixteen bytes of two pieces each, in the order of K's codes.  Returns e.
-template <int D, int NT>
-__device__ __forceinline__ int split_query(const u32x4 (&qf)[D / 16], i32x8 (&t)[NT][D / 64]) {
-  float most = 0.f;
+// qf: the D / 16 pieces of this lane (eight d each), bf16 or (STEP) float16; t[term][MFMA]: sixteen bytes of two pieces each, in the order of K's codes.
+// Returns e.  bf16 elements beyond the float16 range are saturated, as in the kernel for few rows.
+template <int D, int NT, bool STEP>
+__device__ __forceinline__ int split_query(u32x4 (&qf)[D / 16], i32x8 (&t)[NT][D / 64], bool& range) {
+  typedef uint16_t us2 __attribute__((ext_vector_type(2)));
+  auto largest = [&]() {                                // magnitudes compare as integers
+    us2 m{0, 0};
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    const f16x8 h = as_f16x8(qf[s]);
+    for (int s = 0; s < D / 16; ++s)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf((float)h[j]));
+      for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(us2, qf[s][j] & 0x7fff7fffu));
+    return (uint32_t)(m[0] > m[1] ? m[0] : m[1]);
+  };
+  uint32_t bits = largest();
+  float most;
+  if constexpr (STEP) {
+    most = (float)__builtin_bit_cast(f16, (uint16_t)bits);
+  } else {
+    if (bits >= 0x4780) {                               // 65536 and more, infinities, NaN
+      range = true;
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float lo = f16_saturate(__uint_as_float(qf[s][j] << 16)), hi = f16_saturate(__uint_as_float(qf[s][j] & 0xffff0000u));
+          // (65504 is 65280 as bf16, rounded down: the largest bf16 value that float16 holds)
+          qf[s][j] = __float_as_uint(lo) >> 16 | (__float_as_uint(hi) & 0xffff0000u);
+        }
+      bits = largest();
+    }
+    most = __uint_as_float(bits << 16);
   }
   most = max_halves(most);                              // the other half of the row's d
   const uint32_t u = __float_as_uint(most);
   const int e = max((int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), -60);
   const float f = kvq_scale(-e);
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    const f16x8 h = as_f16x8(qf[s]);
+  for (int s = 0; s < D / 16; ++s)
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       float x[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = (float)h[4 * k + j] * f;
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t w = qf[s][2 * k + j / 2];
+        if constexpr (STEP) x[j] = (float)__builtin_bit_cast(f16, (uint16_t)(j & 1 ? w >> 16 : w)) * f;
+        else x[j] = __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16) * f;
+      }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const uint32_t c = kvq_codes4(x[0], x[1], x[2], x[3]);
@@ -610,7 +640,6 @@ __device__ __forceinline__ int split_query(const u32x4 (&qf)[D / 16], i32x8 (&t)
         for (int j = 0; j < 4; ++j) x[j] = (x[j] - y[j]) * 16.f;
       }
     }
-  }
   return e;
 }
 
@@ -664,7 +693,7 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
     constexpr int NQT = decltype(nqt_tag)::value, NPH = 8 / NQT;
     constexpr int NF = 2 * DT, LPW = NF / NQT;          // 1 KiB pieces of a tile, K then V; of those a wave moves
     constexpr int NB = kWideStage<D> / (NPH * NF * 1024);     // buffers: 3 or 6
-    const int32_t* __restrict__ bt = block_table + (size_t)seq_slot[un.b] * max_pages;
+    const int32_t* __restrict__ bt = block_table + (size_t)un.slot * max_pages;
     const int qt = wave / NPH, ph = wave % NPH;
     const bool has_rows = qt * 32 < un.R;               // a wave without query rows only moves data
     const int t_begin = 4 * un.s_lo, t_end = min(4 * un.s_hi, un.n_tiles), n_it = (t_end - t_begin + NPH - 1) / NPH;
@@ -704,9 +733,9 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
     __builtin_amdgcn_sched_barrier(0);
     bool range = false;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) { asm volatile("" : "+v"(qf[s])); qf[s] = query8<STEP>(qf[s], range); }
+    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));
     i32x8 qt8[NT][D / 64];
-    const int q_exp = split_query<D, NT>(qf, qt8);
+    const int q_exp = split_query<D, NT, STEP>(qf, qt8, range);
     f32x16 o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -804,7 +833,7 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
     }
   };
 
-  for_parts<true>(sh, B, s_start, s_row, seq_pos, seq_n, n_add, G, Hkv, [&](const Part& un) {
+  for_parts<true>(sh, B, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G, Hkv, [&](const Part& un) {
     if (tid == 0) s_bad = 0;
     __syncthreads();                                    // LDS of the unit before is no longer read
     if (un.R > 64) run(std::integral_constant<int, 4>{}, un);
