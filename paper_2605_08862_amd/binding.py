@@ -267,10 +267,10 @@ def bs_kv_read(ctx, layer, slot, pos0, n, k_rows, v_rows):
 
 
 def _here(t, dev):
-    """Address of a dense tensor on device `dev` (None: NULL).  The calls without a context launch on the current device's stream: a
+    """Address of a dense tensor on device `dev` (None: NULL; an address: itself).  The calls without a context launch on the current device's stream: a
     tensor of another device is refused."""
-    if t is None:
-        return None
+    if t is None or type(t) is int:
+        return t
     if t.get_device() != dev:
         raise BsError(BS_EINVAL, "tensor on %s, current device cuda:%d" % (t.device, dev))
     if not t.is_contiguous():
@@ -356,12 +356,15 @@ def bs_token_logprobs_workspace_bytes(B, k_max, vocab, n_top):
 
 
 def bs_token_logprobs(B, vocab, logits, draft_len, k_max, tokens, n_tokens, temperature, n_top, logprob, entropy, top_tokens, top_logprobs,
-                      workspace, status=None):
+                      workspace, status=None, workspace_bytes=None):
+    """workspace_bytes: needed where the workspace is given as an address."""
+    if workspace_bytes is None:
+        workspace_bytes = workspace.numel() * workspace.element_size()
     dev = torch.cuda.current_device()
     dtype = BS_F32 if logits.dtype == torch.float32 else BS_BF16 if logits.dtype == torch.bfloat16 else -1
     st = lib().bs_token_logprobs(B, vocab, _here(logits, dev), dtype, _here(draft_len, dev), k_max, _here(tokens, dev), _here(n_tokens, dev), temperature, n_top,
                                  _here(logprob, dev), _here(entropy, dev), _here(top_tokens, dev), _here(top_logprobs, dev), _here(status, dev),
-                                 _here(workspace, dev), workspace.numel() * workspace.element_size(), _stream())
+                                 _here(workspace, dev), workspace_bytes, _stream())
     if st != BS_OK:
         raise BsError(st, "bs_token_logprobs")
 

@@ -244,6 +244,8 @@ class LogprobScorer:
             raise B.BsError(B.BS_ESHAPE, "bs_token_logprobs_workspace_bytes rejected the sizes")
         self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._index = self.workspace.get_device()
+        self._workspace_at, self._workspace_bytes, self._status_at = self.workspace.data_ptr(), nbytes, self.status.data_ptr()
 
     def __call__(self, logits, tokens, n_tokens=None, draft_len=None, temperature=1.0):
         """logits [rows, vocab] (float32 or bf16, packed); tokens [B, k_max + 1]; n_tokens, draft_len [B] or None (all rows).
@@ -251,14 +253,19 @@ class LogprobScorer:
         n, width = tokens.shape
         if n > self.B_max or width > self.k_max + 1 or logits.shape[1] != self.vocab:
             raise B.BsError(B.BS_ESHAPE, "LogprobScorer: sizes exceed those of the workspace")
+        if logits.get_device() != self._index:
+            raise B.BsError(B.BS_EINVAL, "LogprobScorer: logits on %s, workspace on %s" % (logits.device, self.device))
         if draft_len is None and logits.shape[0] < n * width:
             raise B.BsError(B.BS_ESHAPE, "LogprobScorer: fewer rows of logits than tokens")
-        new = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device=self.device)
-        out = {"logprob": new(n, width), "entropy": new(n, width)}
+        lp, h = torch.empty((n, width), device=self.device), torch.empty((n, width), device=self.device)
+        out, at = {"logprob": lp, "entropy": h}, (None, None)
         if self.n_top:
-            out["top_tokens"], out["top_logprobs"] = new(n, width, self.n_top, dtype=torch.int32), new(n, width, self.n_top)
-        B.bs_token_logprobs(n, self.vocab, logits, draft_len, width - 1, tokens, n_tokens, float(temperature), self.n_top, out["logprob"], out["entropy"],
-                            out.get("top_tokens"), out.get("top_logprobs"), self.workspace, self.status)
+            out["top_tokens"] = torch.empty((n, width, self.n_top), dtype=torch.int32, device=self.device)
+            out["top_logprobs"] = torch.empty((n, width, self.n_top), device=self.device)
+            at = out["top_tokens"].data_ptr(), out["top_logprobs"].data_ptr()
+        # (addresses of what was just made need no checks)
+        B.bs_token_logprobs(n, self.vocab, logits, draft_len, width - 1, tokens, n_tokens, temperature, self.n_top, lp.data_ptr(), h.data_ptr(), at[0], at[1],
+                            self._workspace_at, self._status_at, self._workspace_bytes)
         return out
 
     def poll_status(self):
