@@ -572,77 +572,6 @@ __global__ void __launch_bounds__(256, NQ == 1 ? 2 : 1) kvq_attention_kernel(BS_
   });
 }
 
-// Queries as e4m3: q = 2^e (t0 + t1 / 16 + t2 / 256), every term an e4m3 value.  A term has four significant bits, so two hold a bf16 value and three a float16
-// value (what is lost is below 2^-22 of the row's largest element); e is the least with the row's largest element at most 448 * 2^e.  Scores from codes as they are
-// then need no conversion of K: 32 x 32 x 64 products, whose operands take scales 2^x of their own.
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-__device__ __forceinline__ f32x16 mfma_codes(i32x8 a, i32x8 b, f32x16 c, int scale_a, int scale_b) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, scale_a, 0, scale_b);
-#else
-  return c;
-#endif
-}
-__device__ __forceinline__ int scale_byte(int e) { return min(max(e + 127, 1), 254); }
-// qf: the D / 16 pieces of this lane (eight d each), bf16 or (STEP) float16; t[term][MFMA]: sixteen bytes of two pieces each, in the order of K's codes.
-// Returns e.  bf16 elements beyond the float16 range are saturated, as in the kernel for few rows.
-template <int D, int NT, bool STEP>
-__device__ __forceinline__ int split_query(u32x4 (&qf)[D / 16], i32x8 (&t)[NT][D / 64], bool& range) {
-  typedef uint16_t us2 __attribute__((ext_vector_type(2)));
-  auto largest = [&]() {                                // magnitudes compare as integers
-    us2 m{0, 0};
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(us2, qf[s][j] & 0x7fff7fffu));
-    return (uint32_t)(m[0] > m[1] ? m[0] : m[1]);
-  };
-  uint32_t bits = largest();
-  float most;
-  if constexpr (STEP) {
-    most = (float)__builtin_bit_cast(f16, (uint16_t)bits);
-  } else {
-    if (bits >= 0x4780) {                               // 65536 and more, infinities, NaN
-      range = true;
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float lo = f16_saturate(__uint_as_float(qf[s][j] << 16)), hi = f16_saturate(__uint_as_float(qf[s][j] & 0xffff0000u));
-          // (65504 is 65280 as bf16, rounded down: the largest bf16 value that float16 holds)
-          qf[s][j] = __float_as_uint(lo) >> 16 | (__float_as_uint(hi) & 0xffff0000u);
-        }
-      bits = largest();
-    }
-    most = __uint_as_float(bits << 16);
-  }
-  most = max_halves(most);                              // the other half of the row's d
-  const uint32_t u = __float_as_uint(most);
-  const int e = max((int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), -60);
-  const float f = kvq_scale(-e);
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      float x[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t w = qf[s][2 * k + j / 2];
-        if constexpr (STEP) x[j] = (float)__builtin_bit_cast(f16, (uint16_t)(j & 1 ? w >> 16 : w)) * f;
-        else x[j] = __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16) * f;
-      }
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const uint32_t c = kvq_codes4(x[0], x[1], x[2], x[3]);
-        t[n][s / 4][(s % 4) * 2 + k] = (int)c;
-        const f32x4 y = kvq_values4(c);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = (x[j] - y[j]) * 16.f;
-      }
-    }
-  return e;
-}
-
 // Waits until at most N of this wave's requests are in flight (and for its LDS accesses), then for the other waves.
 template <int N> __device__ __forceinline__ void wait_requests() {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -675,7 +604,6 @@ template <int D, bool STEP>
 __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
   constexpr int KS = D / 16, DT = D / 32, RP = 128, CH = D / 4;
   constexpr int DH = D / 2, LDO = DH + 4;               // the accumulators are merged in two halves of the columns
-  constexpr int NT = STEP ? 3 : 2;                      // e4m3 terms of a query: float16 or bf16
   extern __shared__ __align__(16) char lds_raw[];
   __shared__ int s_scan[16], s_bad, s_flag;
   float* const s_o = (float*)lds_raw;                   // [8][32][LDO], on top of the codes
@@ -733,9 +661,7 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
     __builtin_amdgcn_sched_barrier(0);
     bool range = false;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));
-    i32x8 qt8[NT][D / 64];
-    const int q_exp = split_query<D, NT, STEP>(qf, qt8, range);
+    for (int s = 0; s < KS; ++s) { asm volatile("" : "+v"(qf[s])); qf[s] = query8<STEP>(qf[s], range); }
     f32x16 o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -755,8 +681,7 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
       if (has_rows && t < t_end) {
         const char* at = lds_raw + (size_t)(buf * NPH + ph) * NF * 1024 + lane * 16;
         const u32x2 scales = *(const u32x2*)(s_scale + (buf * 8 + wave) * 256);
-        const int ks = (int)(scales[0] >> 23 & 255);    // exponents of powers of two are scale bytes
-        const float vs = __uint_as_float(scales[1]);
+        const float ks = __uint_as_float(scales[0]), vs = __uint_as_float(scales[1]);
         u32x4 kc[DT], vc[DT];
 #pragma unroll
         for (int s = 0; s < DT; ++s) kc[s] = *(const u32x4*)(at + s * 1024);
@@ -765,12 +690,7 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) st[r] = 0.f;
 #pragma unroll
-        for (int u = 0; u < NT; ++u)
-#pragma unroll
-          for (int x = 0; x < D / 64; ++x) {
-            const i32x8 ka{(int)kc[2 * x][0], (int)kc[2 * x][1], (int)kc[2 * x][2], (int)kc[2 * x][3], (int)kc[2 * x + 1][0], (int)kc[2 * x + 1][1], (int)kc[2 * x + 1][2], (int)kc[2 * x + 1][3]};
-            st = mfma_codes(ka, qt8[u][x], st, ks, scale_byte(q_exp - 4 * u));
-          }
+        for (int s = 0; s < KS; ++s) st = mfma32(values8(kc[s / 2][2 * (s % 2)], kc[s / 2][2 * (s % 2) + 1], ks), as_f16x8(qf[s]), st);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int s = 0; s < DT; ++s) vc[s] = *(const u32x4*)(at + (DT + s) * 1024);

@@ -220,3 +220,163 @@ def test_attention_matches_the_oracle(case):
             if r:
                 _close(again[at:at + r], q[at:at + r], x.k[s].read(0, held[b]), x.v[s].read(0, held[b]), ctx[b])
             at += r
+
+
+def _close_on_gpu(x, out, q, slots, ctx, counts):
+    """_close with the reference in float64 on the GPU, from the values that the cache returns."""
+    Hq, Hkv, D = x.dims
+    G, at = Hq // Hkv, 0
+    for s, c, r in zip(slots, ctx, counts):
+        if r == 0:
+            continue
+        t = c + r
+        k, v = (a.double().permute(1, 0, 2) for a in x.cache.read(0, _i32([s]), _i32([0]), _i32([t]), t, t))      # [Hkv, t, D]
+        qd = q[at:at + r].double().view(r, Hkv, G, D).permute(1, 0, 2, 3).reshape(Hkv, r * G, D)
+        hidden = torch.arange(t, device=DEV) > (c + torch.arange(r, device=DEV)).repeat_interleave(G)[:, None]
+        scale = 1.0 / np.sqrt(D)
+        p = torch.softmax((torch.bmm(qd, k.transpose(1, 2).contiguous()) * scale).masked_fill(hidden, -np.inf), -1)
+        back = lambda y: y.view(Hkv, r, G, -1).permute(1, 0, 2, 3).reshape(r, Hq, -1)
+        want, mag = back(torch.bmm(p, v.contiguous())), back(torch.bmm(p, v.abs().contiguous()))
+        most = back((torch.bmm(qd.abs(), k.abs().transpose(1, 2).contiguous()) * scale).masked_fill(hidden, 0.0).amax(-1, keepdim=True))
+        rel = 2.0 ** -11 + 2 * ((D + 8) * 2.0 ** -24 * most + 2.0 ** -18) + (t / 4 + 64) * 2.0 ** -24
+        tol = want.abs() * 2.0 ** -8 + 1.01 * rel * mag + 2.0 ** -25 * v.abs().sum(1).max()
+        err = (out[at:at + r].double() - want).abs()
+        assert bool((err <= tol).all()), (s, float((err / tol).max()))
+        at += r
+
+
+def _filled(Hq, Hkv, D, ctx, counts, seed, bias=0.0):
+    """A cache with context and rows of every sequence, slots in another order than the batch: (Both, slots, queries).  One channel of K is large, with a bias."""
+    rng = np.random.default_rng(seed)
+    n = len(ctx)
+    slots = [int(s) for s in rng.permutation(n)]
+    caps = [0] * n
+    for b in range(n):
+        caps[slots[b]] = max(ctx[b] + counts[b], 1)
+    cache = KvqCache(1, Hq, Hkv, D, n, max(caps), max(counts), device=DEV, page_perm_seed=seed, slot_tokens=caps)
+    x = Both.__new__(Both)
+    x.dims, x.caps, x.cache = (Hq, Hkv, D), caps, cache
+    held = [c + r for c, r in zip(ctx, counts)]
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    rows = lambda size: torch.randn(sum(held), Hkv, D, generator=g, device=DEV).mul_(size).to(torch.bfloat16)
+    k = rows(1.0)
+    k[:, :, 5] = k[:, :, 5] * 8.0 + bias
+    cache.write(0, _i32(slots), _i32([0] * n), _i32(held), max(held), k, rows(0.7))
+    return x, slots, torch.randn(sum(counts), Hq, D, generator=g, device=DEV).to(torch.bfloat16)
+
+
+BIG = [  # Hq, Hkv, D, contexts, rows: what each of the two kernels, the shares and the merges of many parts are for
+    (28, 4, 128, [700, 64, 1300, 0, 33, 129, 2000, 5, 640], [17, 16, 9, 1, 10, 4, 17, 13, 5]),      # blocks of 128 rows, one to four query tiles
+    (16, 2, 64, [500, 90, 0, 77, 1000, 31, 60] * 3, [16, 8, 3, 16, 11, 5, 1] * 3),
+    (28, 4, 128, [20000, 100], [17, 3]),                                                         # few units: many parts of few rows and of many
+    (12, 2, 128, [30001], [1]),
+    (28, 4, 128, [6000] + [60] * 40, [17] + [9] * 40),                                           # one long sequence among short ones
+    (12, 2, 128, [0, 1000, 317], [700, 300, 1]),                                                 # pieces of prompts
+    (8, 8, 64, [40] * 600, [1] * 600),                                                           # more sequences than threads
+    (8, 1, 128, [10 + i % 90 for i in range(4096)], [1] * 4096),                                 # the most sequences
+    (8, 1, 128, [10 + i % 90 for i in range(4096)], [5 + i % 5 for i in range(4096)]),
+]
+
+
+@pytest.mark.parametrize("case", BIG, ids=lambda c: "q%d_kv%d_d%d_b%d_t%d_n%d" % (c[0], c[1], c[2], len(c[3]), max(c[3]), max(c[4])))
+def test_attention_of_larger_batches(case):
+    Hq, Hkv, D, ctx, counts = case
+    x, slots, q = _filled(Hq, Hkv, D, ctx, counts, seed=len(ctx) + D)
+    out = torch.full((sum(counts) + 2, Hq, D), 7.0, dtype=torch.bfloat16, device=DEV)
+    args = (_i32(slots), _i32(ctx), _i32(counts), max(counts))
+    x.cache.attention(0, q, *args, out=out)
+    first = out.clone()
+    some = list(range(len(ctx))) if len(ctx) < 100 else sorted(set(np.random.default_rng(1).integers(0, len(ctx), 25).tolist()) | {0, len(ctx) - 1})
+    row0 = np.concatenate([[0], np.cumsum(counts)])
+    pick = torch.cat([torch.arange(row0[b], row0[b + 1]) for b in some]).to(DEV)
+    _close_on_gpu(x, out[pick], q[pick], [slots[b] for b in some], [ctx[b] for b in some], [counts[b] for b in some])
+    assert bool((out[sum(counts):] == 7.0).all()) and x.cache.poll_status() == 0
+    for _ in range(3):                                                      # the order in which workgroups arrive decides nothing
+        out.fill_(7.0)
+        x.cache.attention(0, q, *args, out=out)
+        assert torch.equal(out, first)
+
+
+@pytest.mark.parametrize("ctx,counts", [([300, 1000], [3, 9]), ([300] * 40, [9] * 40)], ids=["few", "many"])
+def test_scores_beside_a_large_channel(ctx, counts):
+    """A channel that makes most of every score, nearly the same for all keys, leaves the probabilities to small differences: products are summed in
+    float32, not at the place of the largest."""
+    x, slots, q = _filled(28, 4, 128, ctx, counts, seed=12, bias=120.0)
+    out = x.cache.attention(0, q, _i32(slots), _i32(ctx), _i32(counts), max(counts))
+    _close_on_gpu(x, out, q, slots, ctx, counts)
+
+
+@pytest.mark.parametrize("n,counts", [(2, [3, 2]), (40, [9] * 40)], ids=["few", "many"])
+def test_queries_out_of_range_are_saturated(n, counts):
+    x, slots, q = _filled(28, 4, 128, [100] * n, counts, seed=4)
+    args = (_i32(slots), _i32([100] * n), _i32(counts), max(counts))
+    clean = x.cache.attention(0, q, *args)
+    assert x.cache.poll_status() == 0
+    bad = q.clone()
+    bad[1, 5, 7], bad[1, 6, 8], bad[1, 7, 9], bad[2, 0, 0] = float("nan"), float("inf"), float("-inf"), 1e30
+    out = x.cache.attention(0, bad, *args)
+    assert x.cache.poll_status() == B.BS_FAULT_RANGE
+    assert bool(torch.isfinite(out).all()) and torch.equal(out[3:], clean[3:]) and torch.equal(out[0], clean[0]) and torch.equal(out[1, 8:], clean[1, 8:])
+    bad[1, 5, 7] = 0.0                                                       # NaN counts as 0
+    bad[1, 6, 8], bad[1, 7, 9], bad[2, 0, 0] = 65280.0, -65280.0, 65280.0    # the largest bf16 value that float16 holds
+    assert torch.allclose(x.cache.attention(0, bad, *args)[:3].float(), out[:3].float(), rtol=2.0 ** -6, atol=1e-3)
+
+
+@pytest.mark.parametrize("n,ctx,rows", [(1, 9000, 17), (12, 700, 17), (3, 9000, 1)])
+def test_a_bad_page_leaves_its_rows_alone(n, ctx, rows):
+    """Also where the unit is cut into parts; the other sequences are served."""
+    x, slots, q = _filled(28, 4, 128, [ctx] * n, [rows] * n, seed=8)
+    args = (_i32(slots), _i32([ctx] * n), _i32([rows] * n), rows)
+    clean = x.cache.attention(0, q, *args)
+    for page in (x.cache.n_pages, -1):
+        table = x.cache.block_table
+        kept = int(table[slots[-1], 7])
+        table[slots[-1], 7] = page
+        out = torch.full_like(clean, 3.0)
+        x.cache.attention(0, q, *args, out=out)
+        assert x.cache.poll_status() == B.BS_FAULT_KV_PAGES
+        assert torch.equal(out[:-rows], clean[:-rows]) and bool((out[-rows:] == 3.0).all())
+        table[slots[-1], 7] = kept
+        assert torch.equal(x.cache.attention(0, q, *args), clean) and x.cache.poll_status() == 0
+
+
+def test_another_stream_and_two_graphs_on_one_workspace():
+    x, slots, q = _filled(28, 4, 128, [700, 64, 1300, 0, 33, 129, 2000, 5, 640], [17, 16, 9, 1, 10, 4, 17, 13, 5], seed=6)
+    ctx, counts = [700, 64, 1300, 0, 33, 129, 2000, 5, 640], [17, 16, 9, 1, 10, 4, 17, 13, 5]
+    long = (_i32(slots), _i32(ctx), _i32(counts), 17)
+    short = (_i32(slots[:2]), _i32(ctx[:2]), _i32([1, 1]), 1)
+    want, want2 = x.cache.attention(0, q, *long), x.cache.attention(0, q[:2], *short)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = x.cache.attention(0, q, *long)
+    side.synchronize()
+    assert torch.equal(got, want)
+    graphs, outs = [], [torch.zeros_like(want), torch.zeros_like(want2)]
+    for args, qq, o in ((long, q, outs[0]), (short, q[:2].contiguous(), outs[1])):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            x.cache.attention(0, qq, *args, out=o)
+        graphs.append((g, qq))
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        for g, _ in graphs + graphs[:1]:
+            g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want) and torch.equal(outs[1], want2)
+        assert torch.equal(x.cache.attention(0, q, *long), want)             # eager work in between
+    assert x.cache.poll_status() == 0
+
+
+def test_python_checks():
+    x, slots, q = _filled(4, 2, 64, [10, 20], [2, 1], seed=2)
+    args = (_i32(slots), _i32([10, 20]), _i32([2, 1]), 2)
+    for bad in (q.float(), q[:, :2], q.cpu(), q.transpose(1, 2)):
+        with pytest.raises(B.BsError):
+            x.cache.attention(0, bad, *args)
+    with pytest.raises(B.BsError):
+        x.cache.attention(0, q, *args[:3], 3)                                # the workspace is for two rows
+    with pytest.raises(B.BsError):
+        x.cache.attention(0, q, _i32(slots).cpu(), *args[1:])
+    assert x.cache.poll_status() == 0
