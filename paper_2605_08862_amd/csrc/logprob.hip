@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(LogprobArgs a, int se
 }
 
 // Segments of a row: as long as the registers of a workgroup take (kVecs vectors a thread), shorter where there are few rows.  Below kSegLeast words the merge of
-// one more segment costs what its shorter pass saves: 9 rows of 152064 bf16 in segments of 2048 words 22.7 us, 4096 18.8, 8192 16.4, 16384 16.1; 64 rows 23.0, 22.9,
+// one more segment costs what its shorter pass saves: 9 rows of 151936 bf16 words in segments of 2048 words 22.7 us, 4096 18.8, 8192 16.4, 16384 16.1; 64 rows of float32 23.0, 22.9,
 // 22.9, 21.3; 500 rows of 8000 26.9, 20.4, 13.4, 13.5.
 struct Cutting { int seg, segs; };
 constexpr int kSegLeast = 16384, kWanted = 1024;
