@@ -245,15 +245,16 @@ def _close_on_gpu(x, out, q, slots, ctx, counts):
         at += r
 
 
-def _filled(Hq, Hkv, D, ctx, counts, seed, bias=0.0):
-    """A cache with context and rows of every sequence, slots in another order than the batch: (Both, slots, queries).  One channel of K is large, with a bias."""
+def _filled(Hq, Hkv, D, ctx, counts, seed, bias=0.0, cap=40000):
+    """A cache with context and rows of every sequence, slots in another order than the batch: (Both, slots, queries).  One channel of K is large, with a bias.
+    cap: tokens that the block table has room for (of a wide one the kernel for many rows is chosen with fewer sequences)."""
     rng = np.random.default_rng(seed)
     n = len(ctx)
     slots = [int(s) for s in rng.permutation(n)]
     caps = [0] * n
     for b in range(n):
         caps[slots[b]] = max(ctx[b] + counts[b], 1)
-    cache = KvqCache(1, Hq, Hkv, D, n, max(caps), max(counts), device=DEV, page_perm_seed=seed, slot_tokens=caps)
+    cache = KvqCache(1, Hq, Hkv, D, n, max(caps + [cap]), max(counts), device=DEV, page_perm_seed=seed, slot_tokens=caps)
     x = Both.__new__(Both)
     x.dims, x.caps, x.cache = (Hq, Hkv, D), caps, cache
     held = [c + r for c, r in zip(ctx, counts)]
@@ -278,10 +279,11 @@ BIG = [  # Hq, Hkv, D, contexts, rows: what each of the two kernels, the shares 
 ]
 
 
+@pytest.mark.parametrize("cap", [0, 40000], ids=["narrow", "wide"])
 @pytest.mark.parametrize("case", BIG, ids=lambda c: "q%d_kv%d_d%d_b%d_t%d_n%d" % (c[0], c[1], c[2], len(c[3]), max(c[3]), max(c[4])))
-def test_attention_of_larger_batches(case):
+def test_attention_of_larger_batches(case, cap):
     Hq, Hkv, D, ctx, counts = case
-    x, slots, q = _filled(Hq, Hkv, D, ctx, counts, seed=len(ctx) + D)
+    x, slots, q = _filled(Hq, Hkv, D, ctx, counts, seed=len(ctx) + D, cap=cap)
     out = torch.full((sum(counts) + 2, Hq, D), 7.0, dtype=torch.bfloat16, device=DEV)
     args = (_i32(slots), _i32(ctx), _i32(counts), max(counts))
     x.cache.attention(0, q, *args, out=out)
