@@ -290,7 +290,8 @@ typedef struct {
 
 /* Writes rows [n, n_kv_heads, head_dim] bf16 (row_stride elements from one row to the next, at least n_kv_heads * head_dim) to
  * positions pos0[b] .. pos0[b] + n_rows[b] of slot seq_slot[b], n_rows[b] <= n_max.  Positions before pos0 must have been written,
- * positions behind the last row become undefined.  Of sequences with the same slot only the first is written (BS_FAULT_SLOT).
+ * positions behind the last row become undefined.  Of sequences with the same slot only the first is written (BS_FAULT_SLOT); pages that
+ * slots share must not be written through two of them at once.
  * Errors: BS_EINVAL (null, misaligned pages), BS_ESHAPE (head_dim not in {64, 128}, n_kv_heads outside [1, 256], B outside
  * [1, 4096], n_max outside [1, max_pages_per_seq * BS_PAGE_TOKENS], row_stride too small, a launch of more than 2^23 pages), BS_EHIP. */
 bs_status bs_kvq_write(const bs_kvq_desc* kv, int B, const int32_t* seq_slot /*[B]*/, const int32_t* pos0 /*[B]*/,
@@ -304,7 +305,7 @@ bs_status bs_kvq_read(const bs_kvq_desc* kv, int B, const int32_t* seq_slot, con
  * q_stride elements from one row to the next, at least n_q_heads * head_dim) at positions ctx_len[b] .. ctx_len[b] + q_len[b];
  * their own K/V rows have been written before.  Row i sees positions 0 .. ctx_len[b] + i:
  *   out = softmax(q K^T / sqrt(head_dim)) V,   out: bf16 [rows, n_q_heads, head_dim], packed.
- * Query head j reads KV head j / (n_q_heads / n_kv_heads).  Products run on float16 operands (queries beyond +-65504 are
+ * Slots may repeat.  Query head j reads KV head j / (n_q_heads / n_kv_heads).  Products run on float16 operands (queries beyond +-65504 are
  * saturated, NaN becomes 0, BS_FAULT_RANGE) with float32 accumulation and softmax.
  * workspace (dev, 256-byte aligned, at least bs_kvq_workspace_bytes of the same n_q_heads, n_kv_heads, head_dim and of a q_max no
  * smaller) is zero-filled once before its first use; calls that share one must not overlap in time.
@@ -341,7 +342,7 @@ bs_status bs_kvq_bind(bs_ctx* ctx, const bs_kvq_desc* layers /*host[L] or NULL*/
  * n_tokens is out of range (BS_FAULT_DRAFT_LEN; a draft_len outside [0, k_max] counts no rows).  status: as above.
  * workspace (dev, 256-byte aligned, at least bs_token_logprobs_workspace_bytes of the same vocab and n_top and of B and k_max no smaller) is zero-filled
  * once before its first use; calls that share one must not overlap in time.
- * Errors: BS_EINVAL (null, temperature or its reciprocal not in (0, inf), bad dtype, logits not aligned to their elements), BS_ESHAPE (vocab < 2 or > 2^20, n_top outside
+ * Errors: BS_EINVAL (null, temperature not in [1e-38, inf), bad dtype, logits not aligned to their elements), BS_ESHAPE (vocab < 2 or > 2^20, n_top outside
  * [0, 32] or above vocab, B or k_max + 1 outside [1, 4096], more than 2^16 rows), BS_ECAPACITY (workspace too small), BS_EHIP. */
 size_t bs_token_logprobs_workspace_bytes(int B, int k_max, int vocab, int n_top);   /* 0 on invalid arguments */
 bs_status bs_token_logprobs(int B, int vocab, const void* logits, int logits_dtype, const int32_t* draft_len /*[B] or NULL*/,

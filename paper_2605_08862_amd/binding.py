@@ -278,6 +278,15 @@ def _here(t, dev):
     return t.data_ptr()
 
 
+def _ints(t, n, dev):
+    """Address of at least n int32 words on device `dev` (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.numel() < n:
+        raise BsError(BS_EINVAL, "%d int32 words are expected, not %d of %s" % (n, t.numel(), t.dtype))
+    return _here(t, dev)
+
+
 def _rows(t, width, dev):
     """(address, elements from one row to the next) of packed rows [n, ..., ...] whose inner dimensions are dense."""
     if t.get_device() != dev:
@@ -311,7 +320,9 @@ def _kvq_copy(name, desc, B, seq_slot, pos0, n_rows, n_max, k_rows, v_rows, stat
     v, v_stride = _rows(v_rows, width, dev)
     if stride != v_stride or k_rows.shape[0] != v_rows.shape[0]:
         raise BsError(BS_EINVAL, name + ": K and V rows must have the same number and stride")
-    st = getattr(lib(), name)(C.byref(desc), B, _here(seq_slot, dev), _here(pos0, dev), _here(n_rows, dev), n_max, k, v, stride, _here(status, dev), _stream())
+    if k_rows.shape[0] == 0:              # nothing is there for any sequence (an empty tensor has no address)
+        return
+    st = getattr(lib(), name)(C.byref(desc), B, _ints(seq_slot, B, dev), _ints(pos0, B, dev), _ints(n_rows, B, dev), n_max, k, v, stride, _ints(status, 1, dev), _stream())
     if st != BS_OK:
         raise BsError(st, name)
 
@@ -333,8 +344,10 @@ def bs_kvq_attention(desc, B, seq_slot, ctx_len, q_len, q_max, n_q_heads, q, out
     address, stride = _rows(q, n_q_heads * desc.head_dim, dev)
     if out.dtype != torch.bfloat16 or out.numel() < q.numel():
         raise BsError(BS_EINVAL, "bs_kvq_attention: out is bfloat16, with a row for every row of q")
-    st = lib().bs_kvq_attention(C.byref(desc), B, _here(seq_slot, dev), _here(ctx_len, dev), _here(q_len, dev), q_max, n_q_heads, address, stride, _here(out, dev),
-                                _here(status, dev), _here(workspace, dev), workspace.numel() * workspace.element_size(), _stream())
+    if q.shape[0] == 0:
+        return
+    st = lib().bs_kvq_attention(C.byref(desc), B, _ints(seq_slot, B, dev), _ints(ctx_len, B, dev), _ints(q_len, B, dev), q_max, n_q_heads, address, stride, _here(out, dev),
+                                _ints(status, 1, dev), _here(workspace, dev), workspace.numel() * workspace.element_size(), _stream())
     if st != BS_OK:
         raise BsError(st, "bs_kvq_attention")
 
@@ -344,7 +357,7 @@ def bs_kvq_bind_bytes(ctx):
 
 
 def bs_kvq_bind(ctx, descs, workspace):
-    """descs: list of bs_kvq_desc, one per layer (None unbinds)."""
+    """descs: list of bs_kvq_desc, one for each of the model's layers (None unbinds)."""
     if descs is None:
         _check(ctx, lib().bs_kvq_bind(ctx, None, None, 0))
         return
@@ -360,9 +373,11 @@ def bs_token_logprobs(B, vocab, logits, draft_len, k_max, tokens, n_tokens, temp
     """workspace_bytes: needed where the workspace is given as an address."""
     if workspace_bytes is None:
         workspace_bytes = workspace.numel() * workspace.element_size()
+    if logits.shape[-1] != vocab:
+        raise BsError(BS_ESHAPE, "bs_token_logprobs: rows of %d logits, %d expected" % (logits.shape[-1], vocab))
     dev = torch.cuda.current_device()
     dtype = BS_F32 if logits.dtype == torch.float32 else BS_BF16 if logits.dtype == torch.bfloat16 else -1
-    st = lib().bs_token_logprobs(B, vocab, _here(logits, dev), dtype, _here(draft_len, dev), k_max, _here(tokens, dev), _here(n_tokens, dev), temperature, n_top,
+    st = lib().bs_token_logprobs(B, vocab, _here(logits, dev), dtype, _ints(draft_len, B, dev), k_max, _ints(tokens, B * (k_max + 1), dev), _ints(n_tokens, B, dev), temperature, n_top,
                                  _here(logprob, dev), _here(entropy, dev), _here(top_tokens, dev), _here(top_logprobs, dev), _here(status, dev),
                                  _here(workspace, dev), workspace_bytes, _stream())
     if st != BS_OK:

@@ -835,6 +835,7 @@ bs_status bs_kvq_bind(bs_ctx* c, const bs_kvq_desc* layers, void* workspace, siz
   if (!c) return BS_EINVAL;
   if (!layers) { c->kvq.clear(); c->verify_pending = false; return BS_OK; }
   if (c->s.dtype != BS_BF16) return fail(c, BS_EINVAL, "bs_kvq_bind: float32 models have no 8-bit cache");
+  if (!kvq_heads_ok(c->s.Hq, c->s.Hkv, c->s.D)) return fail(c, BS_ESHAPE, "bs_kvq_bind: heads that bs_kvq_attention does not take");
   if (!workspace || ((uintptr_t)workspace & 255)) return fail(c, BS_EINVAL, "bs_kvq_bind: workspace null or not on 256 bytes");
   for (int l = 0; l < c->s.L; ++l) {
     const bs_kvq_desc& d = layers[l];
@@ -868,7 +869,7 @@ bs_status bs_token_logprobs(int B, int vocab, const void* logits, int logits_dty
                             float* top_logprobs, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
   if (!logits || !tokens || !logprob || !workspace || (n_top > 0 && (!top_tokens || !top_logprobs))) return BS_EINVAL;
   if (logits_dtype != BS_F32 && logits_dtype != BS_BF16) return BS_EINVAL;
-  if (!(temperature > 0.f) || !(1.0f / temperature > 0.f) || !(1.0f / temperature <= 3.4028235e38f) || ((uintptr_t)logits & (logits_dtype == BS_F32 ? 3 : 1)) || ((uintptr_t)workspace & 255)) return BS_EINVAL;
+  if (!(temperature >= 1e-38f) || !(temperature <= 3.4028235e38f) || ((uintptr_t)logits & (logits_dtype == BS_F32 ? 3 : 1)) || ((uintptr_t)workspace & 255)) return BS_EINVAL;
   const size_t need = bs_token_logprobs_workspace_bytes(B, k_max, vocab, n_top);
   if (need == 0) return BS_ESHAPE;
   if (workspace_bytes < need) return BS_ECAPACITY;

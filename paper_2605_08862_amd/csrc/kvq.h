@@ -82,7 +82,7 @@ void launch_kvq_attention(const KvqView& kv, const KvqSeqs& q, int Hq, const voi
                           hipStream_t st);
 // of a verify step: float16 queries [rows][Hq][D], output in chunk order (act_index, out_ld)
 void launch_kvq_step_attention(const KvqView& kv, const KvqSeqs& q, int Hq, const void* qrows, void* out, int out_ld, int32_t* status, void* workspace, hipStream_t st);
-// Whether the lengths of all units (at most 92 for each step of 128 tokens) can be counted in 32 bits.
+// Whether the lengths of all units (at most 96 for each step of 128 tokens and 128 rows) can be counted in 32 bits.
 inline bool kvq_attention_counts(int B, int Hkv, int G, int max_pages, int q_max) {
   return (int64_t)B * Hkv * (max_pages / 2 + 1) <= ((int64_t)1 << 24) / ((int64_t)q_max * G / 128 + 1);
 }

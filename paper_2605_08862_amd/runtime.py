@@ -53,6 +53,8 @@ class Engine:
         """max_ctx: token capacity of every slot; slot_tokens (optional, one entry per slot) gives every slot its own
         capacity instead, so that a ragged batch only takes the pages it needs (block-table entries beyond a slot's
         pages are -1).  kv_bits = 8 (bf16 models): the cache holds 8 bits per element (KvqCache, bs_kvq_bind)."""
+        if kv_bits not in (16, 8) or (kv_bits == 8 and desc["dtype"] != B.BS_BF16):
+            raise B.BsError(B.BS_EINVAL, "kv_bits is 16 or, for bf16 models, 8")
         self.desc = dict(desc)
         self.device = torch.device(device)
         self.cdesc = B.make_desc(desc)
@@ -185,7 +187,7 @@ class Engine:
 class KvqCache:
     """Owns a KV cache in 8 bits (pages, scales and block table of every layer, attention workspace) and forwards to bs_kvq_*.
     Slots, capacities and page permutation as in Engine.  Rows are packed in batch order; n_max / q_max bound the rows of a
-    sequence, which are on the device.  `status` (one int32 on the device) collects BS_FAULT_* bits until poll_status."""
+    sequence, which are on the device.  One attention call at a time: the workspace is shared.  `status` (one int32 on the device) collects BS_FAULT_* bits until poll_status."""
 
     def __init__(self, n_layers, n_q_heads, n_kv_heads, head_dim, n_slots, max_ctx, q_max, device="cuda:0", page_perm_seed=None,
                  slot_tokens=None, block_table=None, n_pages=0):
@@ -234,7 +236,8 @@ class KvqCache:
 
 
 class LogprobScorer:
-    """Owns the workspace of bs_token_logprobs for up to B_max sequences of k_max + 1 rows."""
+    """Owns the workspace of bs_token_logprobs for up to B_max sequences of k_max + 1 rows.  The tokens, counts and logits of an
+    accept call can be passed on; `status` collects BS_FAULT_* bits until poll_status.  One call at a time: the workspace is shared."""
 
     def __init__(self, B_max, k_max, vocab, n_top, device="cuda:0"):
         self.B_max, self.k_max, self.vocab, self.n_top = B_max, k_max, vocab, n_top

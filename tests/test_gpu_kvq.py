@@ -379,6 +379,33 @@ def test_python_checks():
             x.cache.attention(0, bad, *args)
     with pytest.raises(B.BsError):
         x.cache.attention(0, q, *args[:3], 3)                                # the workspace is for two rows
-    with pytest.raises(B.BsError):
-        x.cache.attention(0, q, _i32(slots).cpu(), *args[1:])
+    for i in range(3):                                                       # on the host, of another type, too short
+        for bad in (args[i].cpu(), args[i].long(), args[i][:1]):
+            with pytest.raises(B.BsError):
+                x.cache.attention(0, q, *(args[:i] + (bad,) + args[i + 1:])) if i else B.bs_kvq_attention(x.cache.desc[0], 2, bad, *args[1:], 4, q, torch.empty_like(q), x.cache.workspace)
+    k = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device=DEV)
+    for bad in (k[:2], k.float(), k[:, :1], k.cpu()):
+        with pytest.raises(B.BsError):
+            x.cache.write(0, *args, k, bad)
     assert x.cache.poll_status() == 0
+
+
+def test_batches_without_rows_and_repeated_slots():
+    """Padded entries keep whatever slot and context they have; a batch of them alone does nothing.  Reads and attention take a slot twice."""
+    x, slots, q = _filled(28, 4, 128, [300, 20], [3, 2], seed=9)
+    none = torch.empty(0, 28, 128, dtype=torch.bfloat16, device=DEV)
+    pad = (_i32([-1, 99]), _i32([-5, 2 ** 30]), _i32([0, 0]))
+    assert x.cache.attention(0, none, *pad, 3).shape == (0, 28, 128)
+    x.cache.write(0, *pad, 3, none[:, :4], none[:, :4])
+    out = torch.full_like(q, 3.0)
+    assert bool((x.cache.attention(0, q, *pad, 3, out=out) == 3.0).all())
+    k = torch.ones(5, 4, 128, dtype=torch.bfloat16, device=DEV)
+    x.cache.write(0, *pad, 3, k, k)
+    want = x.cache.attention(0, q, _i32(slots), _i32([300, 20]), _i32([3, 2]), 3)
+    s = slots[0]
+    twice = x.cache.attention(0, torch.cat([q[:3], q[1:3], q[:1]]), _i32([s, 99, s, s]), _i32([300, 2 ** 30, 301, 300]), _i32([3, 0, 2, 1]), 3)
+    assert torch.equal(twice[:3], want[:3]) and x.cache.poll_status() == 0
+    assert torch.allclose(twice[3:5].float(), want[1:3].float(), rtol=2.0 ** -6, atol=2.0 ** -7) and torch.allclose(twice[5].float(), want[0].float(), rtol=2.0 ** -6, atol=2.0 ** -7)
+    a, _ = x.cache.read(0, _i32([s, s, s]), _i32([10, 0, 64]), _i32([100, 110, 3]), 110, 213)
+    b, _ = x.cache.read(0, _i32([s]), _i32([0]), _i32([110]), 110, 110)
+    assert torch.equal(a[:100], b[10:]) and torch.equal(a[100:210], b) and torch.equal(a[210:], b[64:67]) and x.cache.poll_status() == 0

@@ -133,3 +133,67 @@ def test_faults_and_optional_outputs():
     B.bs_token_logprobs(3, V, z, None, 2, _i32(tokens[:3]), None, 1.0, 0, lp, None, None, None, s.workspace)   # no status, no entropy, no alternatives
     want = torch.log_softmax(z.double(), -1).view(3, 3, V).gather(2, torch.as_tensor(tokens[:3], device=DEV)[..., None])[..., 0]
     assert torch.allclose(lp.double(), want, atol=1e-5)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_largest_vocabulary(dtype):
+    """Rows of 64 segments; one in which more elements of every segment are equal than its list of candidates holds, and so are more of their best."""
+    V, n_top = 2 ** 20, 32
+    rng = np.random.default_rng(20)
+    z = torch.from_numpy(rng.normal(0, 2.5, (4, V)).astype(np.float32))
+    z[1] = 1.0
+    z[2] = -INF
+    z[2, rng.integers(0, V, 40)] = 2.0
+    z = z.to(dtype)
+    tokens = np.array([[0, V - 1], [12345, 7]])
+    s = LogprobScorer(2, 1, V, n_top, device=DEV)
+    _check(s(z.to(DEV), _i32(tokens)), z, tokens, [2, 2], [1, 1], 1.0, n_top)
+    assert s.poll_status() == 0
+
+
+@pytest.mark.parametrize("temperature", [1e-38, 1e-3, 3e38])
+def test_extreme_temperatures(temperature):
+    t = float(np.float32(temperature))
+    z = torch.from_numpy(np.random.default_rng(3).normal(0, 2.5, (3, 200)).astype(np.float32))
+    tokens = np.array([[int(z[0].argmax())], [3], [4]])
+    _check(LogprobScorer(3, 0, 200, 3, device=DEV)(z.to(DEV), _i32(tokens), temperature=t), z, tokens, [1] * 3, [0] * 3, t, 3)
+
+
+def test_captured_and_on_another_stream():
+    """A graph sees new logits, tokens and counts in the same places; eager calls on the same workspace in between."""
+    V, n_top, draft_len, n_tokens = 40001, 8, [3, 0, 2], [4, 1, 2]
+    rng = np.random.default_rng(11)
+    s = LogprobScorer(3, 3, V, n_top, device=DEV)
+    new = lambda: torch.from_numpy(rng.normal(0, 2.5, (8, V)).astype(np.float32)).to(DEV)
+    z, tokens, nt, dl = new(), rng.integers(0, V, (3, 4)), _i32(n_tokens), _i32(draft_len)
+    tok = _i32(tokens)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out = s(z, tok, nt, dl)
+    side.synchronize()
+    _check(out, z, tokens, n_tokens, draft_len, 1.0, n_top)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = s(z, tok, nt, dl)
+    for _ in range(3):
+        z.copy_(new())
+        for v in out.values():
+            v.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        _check(out, z, tokens, n_tokens, draft_len, 1.0, n_top)
+        eager = s(z, tok, nt, dl)
+        assert all(torch.equal(out[k], eager[k]) for k in out)
+    assert s.poll_status() == 0
+
+
+def test_python_checks():
+    s = LogprobScorer(2, 1, 100, 3, device=DEV)
+    z, tokens = torch.zeros(4, 100, device=DEV), _i32([[1, 2], [3, 4]])
+    for call in (lambda: s(z[:3], tokens), lambda: s(z[:, :99], tokens), lambda: s(z.half(), tokens), lambda: s(z.cpu(), tokens), lambda: s(z, tokens.long()), lambda: s(z, tokens.cpu()),
+                 lambda: s(z, tokens, n_tokens=_i32([1])), lambda: s(z, tokens, draft_len=_i32([1])), lambda: s(z, _i32([[1, 2, 3]])), lambda: s(z, _i32([[1], [2], [3]])),
+                 lambda: s(z, tokens, temperature=0.0), lambda: s(z, tokens, temperature=float("nan")), lambda: s(z, tokens, temperature=INF), lambda: s(z, tokens, temperature=1e-39)):
+        with pytest.raises(B.BsError):
+            call()
+    assert s.poll_status() == 0
