@@ -572,12 +572,14 @@ __device__ __forceinline__ void copy_to_lds(const uint8_t* src, char* dst) {
 // w has phase w % NPH of query tile w / NPH, so that the waves of a SIMD (w % 4) are of different query tiles.  The waves of a phase share a tile of codes in LDS:
 // the memory pipeline copies it there (global -> LDS loads, a share of the 1 KiB pieces by each wave), NB buffers for each phase, NB - 1 tiles in flight and one
 // barrier per tile.
-// What bounds it: two query tiles, memory; four, that the softmax's vector instructions and the conversions (700 cycles of a tile) and the matrix instructions (512) of
-// the two waves of a SIMD overlap in part only.  7B heads, 32 sequences of 8192 tokens (memory 57 us), 9 rows 66 us, 13 rows 90, 17 rows 100.  Two tiles per barrier, a tile
-// of K read ahead, requests behind the scores: the same or slower; twelve waves with three phases: 12 us more; scores of the next tile multiplied while this one's
-// become probabilities: 10 us more; two query tiles in a wave, which halves the conversions, with queries in LDS: 17 rows 101, 9 rows 70.  Scores from 8-bit products
-// (queries split into e4m3 terms) took 17 rows to 96 us, but the matrix unit sums those eight at a time at the place of the largest and drops what is below 2^-13 of it:
-// K with one large channel is then read wrongly.
+// What bounds it: two query tiles, memory; four, that matrix and vector instructions of the two waves of a SIMD overlap in part only.  7B heads, 32 sequences of 8192
+// tokens (memory 57 us), 9 rows 66 us, 13 rows 90, 17 rows 100 .. 105.  Of the latter, with parts left out: the way to the first tile and the merges 22, copying the tiles
+// alone 69, matrix instructions alone 84 (half of their nominal rate, as a large matrix product has it too), everything but them 87, everything but the softmax 90,
+// everything but the conversions 100.  Two tiles per barrier, a tile of K read ahead, requests behind the scores: the same or slower; twelve waves with three phases:
+// 12 us more; scores of the next tile multiplied while this one's become probabilities: 10 us more; the two waves of a SIMD held half a tile apart by barriers: 10 us more;
+// two query tiles in a wave, which halves the conversions, with queries in LDS: 17 rows 101, 9 rows 70.  Scores from 8-bit products (queries split into e4m3 terms) took
+// 17 rows to 96 us, but the matrix unit sums those eight at a time at the place of the largest and drops what is below 2^-13 of it: K with one large channel is then
+// read wrongly.
 template <int D> constexpr int kWideStage = 96 * 1024 * D / 128;
 constexpr int kWideScales = 6 * 8 * 256;                // [buffers][waves] K and V scale in the first two words
 template <int D, bool STEP>
