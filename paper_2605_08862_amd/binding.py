@@ -266,6 +266,9 @@ def bs_kv_read(ctx, layer, slot, pos0, n, k_rows, v_rows):
     _check(ctx, lib().bs_kv_read(ctx, layer, slot, pos0, n, _ptr(k_rows), _ptr(v_rows), _stream()))
 
 
+_I32, _BF16 = torch.int32, torch.bfloat16
+
+
 def _here(t, dev):
     """Address of a dense tensor on device `dev` (None: NULL; an address: itself).  The calls without a context launch on the current device's stream: a
     tensor of another device is refused."""
@@ -279,16 +282,20 @@ def _here(t, dev):
 
 
 def _ints(t, n, dev):
-    """Address of at least n int32 words on device `dev` (None: NULL)."""
-    if t is None:
-        return None
-    if t.dtype != torch.int32 or t.numel() < n:
+    """Address of at least n int32 words on device `dev` (None: NULL; an address: itself)."""
+    if t is None or type(t) is int:
+        return t
+    if t.dtype is _I32 and t.numel() >= n and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    if t.dtype is not _I32 or t.numel() < n:
         raise BsError(BS_EINVAL, "%d int32 words are expected, not %d of %s" % (n, t.numel(), t.dtype))
     return _here(t, dev)
 
 
 def _rows(t, width, dev):
     """(address, elements from one row to the next) of packed rows [n, ..., ...] whose inner dimensions are dense."""
+    if t.dtype is _BF16 and t.get_device() == dev and t.is_contiguous() and t.shape[0] * width == t.numel():
+        return t.data_ptr(), width
     if t.get_device() != dev:
         raise BsError(BS_EINVAL, "tensor on %s, current device cuda:%d" % (t.device, dev))
     if t.dtype != torch.bfloat16:
@@ -296,8 +303,6 @@ def _rows(t, width, dev):
     n = t.shape[0]
     if n * width != t.numel():
         raise BsError(BS_ESHAPE, "rows of %s elements, %d expected" % (tuple(t.shape[1:]), width))
-    if t.is_contiguous():
-        return t.data_ptr(), width
     inner = 1
     for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
         if size != 1 and stride != inner:

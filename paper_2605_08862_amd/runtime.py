@@ -260,7 +260,8 @@ class LogprobScorer:
             raise B.BsError(B.BS_EINVAL, "LogprobScorer: logits on %s, workspace on %s" % (logits.device, self.device))
         if draft_len is None and logits.shape[0] < n * width:
             raise B.BsError(B.BS_ESHAPE, "LogprobScorer: fewer rows of logits than tokens")
-        lp, h = torch.empty((n, width), device=self.device), torch.empty((n, width), device=self.device)
+        lp = torch.empty((n, width), device=self.device)
+        h = torch.empty_like(lp)
         out, at = {"logprob": lp, "entropy": h}, (None, None)
         if self.n_top:
             out["top_tokens"] = torch.empty((n, width, self.n_top), dtype=torch.int32, device=self.device)
