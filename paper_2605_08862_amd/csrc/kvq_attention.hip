@@ -69,11 +69,14 @@ struct Shares {
   }
 };
 
-// Called by all threads.  s_start, s_row [B + 1]: where every sequence begins, and its first packed row; s_scan: 2 words for each wave.
+// A sequence that the thread which counted it leaves for the others: the one that this workgroup's share begins in.
+struct Seq { int b, first, end, row0, n, c, slot; };
+
+// Called by all threads.  s_start, s_row [B + 1]: where every sequence begins, and its first packed row; s_scan: 2 words for each wave; s_seq: see above.
 // A share is no shorter than `least`, and longer than a step, so that every share between two others of a unit has a step of it.
 template <int THREADS, bool WIDE>
 __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
-                                              int n_max, int B, int n_slots, int max_pages, Group G, int Hkv, int least, int* s_start, int* s_row, int* s_scan,
+                                              int n_max, int B, int n_slots, int max_pages, Group G, int Hkv, int least, int* s_start, int* s_row, int* s_scan, Seq* s_seq,
                                               int32_t* __restrict__ status) {
   constexpr int NW = THREADS / 64, RP = kBlock<WIDE>;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -82,10 +85,10 @@ __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_sl
   while (subs < 64 && 2 * subs * B <= THREADS) subs *= 2;
   const int per = subs > 1 ? 1 : (B + THREADS - 1) / THREADS, sub = tid & (subs - 1), at = tid / subs;
   const int lo = min(at * per, B), hi = min(lo + per, B);
-  int cost = 0, rows = 0, fault = 0;
+  int cost = 0, rows = 0, fault = 0, n = 0, slot = 0, c = 0;
   for (int b = lo; b < hi; ++b) {
     if (sub == 0) { s_start[b] = cost; s_row[b] = rows; }
-    const int n = seq_n[b] + n_add, slot = seq_slot[b], c = seq_pos[b];
+    n = seq_n[b] + n_add; slot = seq_slot[b]; c = seq_pos[b];
     if (n < 0 || n > n_max) { fault |= BS_FAULT_DRAFT_LEN; continue; }
     if (n == 0) continue;
     if (sub == 0) rows += n;
@@ -112,15 +115,25 @@ __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_sl
     if (w < wave) { bs += s_scan[w]; br += s_scan[NW + w]; }
     total += s_scan[w];
   }
-  if (sub == 0)
-    for (int b = lo; b < hi; ++b) { s_start[b] += bs; s_row[b] += br; }
-  if (tid == 0) s_start[B] = total;
-  __syncthreads();
   Shares sh;
   sh.total = __builtin_amdgcn_readfirstlane(total);
   sh.W = __builtin_amdgcn_readfirstlane(min((int)gridDim.x, max(1, total / least)));
-  sh.per = ((unsigned long long)sh.total << 16) / (unsigned)sh.W;
+  sh.per = (unsigned long long)((double)sh.total * 65536.0 / (double)sh.W);    // the same in every workgroup; (W - 1) per is below the total
   sh.inv = (float)sh.W / (float)max(sh.total, 1);
+  if (sub == 0) {
+    const int p0 = sh.bound(blockIdx.x);
+    for (int b = lo; b < hi; ++b) {
+      const int first = s_start[b] + bs, row0 = s_row[b] + br, end = b + 1 < hi ? s_start[b + 1] + bs : bs + cost;
+      s_start[b] = first;
+      s_row[b] = row0;
+      if (first <= p0 && p0 < end) {
+        if (per > 1) { n = seq_n[b] + n_add; slot = seq_slot[b]; c = seq_pos[b]; }
+        *s_seq = Seq{b, first, end, row0, n, c, slot};
+      }
+    }
+  }
+  if (tid == 0) s_start[B] = total;
+  __syncthreads();
   return sh;
 }
 
@@ -157,20 +170,20 @@ __device__ __forceinline__ void enter_sequence(Unit<WIDE>& u, const int* s_start
   u.h = u.qb = 0;
   fill_unit<WIDE>(u, G);
 }
-// The unit that p (below the total) lies in.
+// The unit that p lies in, of the sequence that p lies in.
 template <bool WIDE>
-__device__ __forceinline__ Unit<WIDE> unit_at(int p, int B, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
-                                        Group G, int Hkv) {
+__device__ __forceinline__ Unit<WIDE> unit_at(int p, const Seq& s, Group G, int Hkv) {
   Unit<WIDE> u;
-  int lo = 0, hi = B;                                   // largest b with s_start[b] <= p (sequences without units are passed over)
-  while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_start[mid] <= p) lo = mid; else hi = mid; }
-  u.b = lo;
-  enter_sequence<WIDE>(u, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G);
-  const int all = __builtin_amdgcn_readfirstlane(s_start[u.b + 1]) - u.first, head = u.blocks == 1 ? u.end() - u.first : all / Hkv;
+  auto same = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  u.b = same(s.b); u.n = same(s.n); u.c = same(s.c); u.slot = same(s.slot); u.row0 = same(s.row0); u.first = same(s.first);
+  u.blocks = (u.n * G.g + kBlock<WIDE> - 1) / kBlock<WIDE>;
+  u.h = u.qb = 0;
+  fill_unit<WIDE>(u, G);
+  const int head = u.blocks == 1 ? u.end() - u.first : (same(s.end) - u.first) / Hkv;
   int h = min(Hkv - 1, (int)((float)(p - u.first) / (float)head));
   while (h > 0 && h * head > p - u.first) --h;
   while (h + 1 < Hkv && (h + 1) * head <= p - u.first) ++h;
-  u.h = __builtin_amdgcn_readfirstlane(h);
+  u.h = same(h);
   u.first += u.h * head;
   while (u.end() <= p) { u.first = u.end(); ++u.qb; fill_unit<WIDE>(u, G); }
   return u;
@@ -214,11 +227,11 @@ __device__ __forceinline__ Part part_of(const Unit<WIDE>& u, const Shares& sh, i
 // Calls f(part) for every part of this workgroup's share.
 template <bool WIDE, typename F>
 __device__ __forceinline__ void for_parts(const Shares& sh, int B, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos,
-                                          const int32_t* __restrict__ seq_n, int n_add, Group G, int Hkv, const F& f) {
+                                          const int32_t* __restrict__ seq_n, int n_add, Group G, int Hkv, const Seq& s_seq, const F& f) {
   const int w = blockIdx.x;
   if (w >= sh.W || sh.total == 0) return;
   const int p0 = __builtin_amdgcn_readfirstlane(sh.bound(w)), p1 = __builtin_amdgcn_readfirstlane(sh.bound(w + 1));
-  Unit<WIDE> u = unit_at<WIDE>(p0, B, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G, Hkv);
+  Unit<WIDE> u = unit_at<WIDE>(p0, s_seq, G, Hkv);
   int s_lo = u.cut(p0);
   while (true) {
     const bool last = u.end() >= p1;
@@ -417,6 +430,7 @@ __global__ void __launch_bounds__(256, 2) kvq_attention_kernel(BS_KVQ_PARAMS) {
   constexpr int LDO = D + 4;                            // row stride (floats) of an accumulator in LDS
   extern __shared__ __align__(16) char lds_raw[];
   __shared__ int s_scan[8], s_flag;
+  __shared__ Seq s_seq;
   u32x4* const s_q = (u32x4*)lds_raw;                   // [KS][64] query fragments; behind a unit's last product, the waves' accumulators
   float* const s_o = (float*)lds_raw;                   // [4][32][LDO]
   float* const s_m = s_o + 4 * 32 * LDO;                // [4][32]
@@ -426,8 +440,8 @@ __global__ void __launch_bounds__(256, 2) kvq_attention_kernel(BS_KVQ_PARAMS) {
   const int tid = threadIdx.x, w_id = blockIdx.x;
   const Group G{g_n, g_recip};
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, ln = lane & 31, lg = lane >> 5;
-  const Shares sh = find_shares<256, false>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, least, s_start, s_row, s_scan, status);
-  for_parts<false>(sh, B, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G, Hkv, [&](const Part& un) {
+  const Shares sh = find_shares<256, false>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, least, s_start, s_row, s_scan, &s_seq, status);
+  for_parts<false>(sh, B, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G, Hkv, s_seq, [&](const Part& un) {
     const int32_t* __restrict__ bt = block_table + (size_t)un.slot * max_pages;
     const int t0 = 4 * un.s_lo + wave, t_end = min(4 * un.s_hi, un.n_tiles);
     const int n_my = t0 < t_end ? (t_end - t0 + 3) / 4 : 0, t_last = t0 + (n_my - 1) * 4;
@@ -588,6 +602,7 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
   constexpr int DH = D / 2, LDO = DH + 4;               // the accumulators are merged in two halves of the columns
   extern __shared__ __align__(16) char lds_raw[];
   __shared__ int s_scan[16], s_bad, s_flag;
+  __shared__ Seq s_seq;
   float* const s_o = (float*)lds_raw;                   // [8][32][LDO], on top of the codes
   char* const s_scale = lds_raw + kWideStage<D>;
   float* const s_m = (float*)(s_scale + kWideScales);   // [8][32]
@@ -597,7 +612,7 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
   const int tid = threadIdx.x, w_id = blockIdx.x;
   const Group G{g_n, g_recip};
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, ln = lane & 31, lg = lane >> 5;
-  const Shares sh = find_shares<512, true>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, least, s_start, s_row, s_scan, status);
+  const Shares sh = find_shares<512, true>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, least, s_start, s_row, s_scan, &s_seq, status);
 
   auto run = [&](auto nqt_tag, const Part& un) {
     constexpr int NQT = decltype(nqt_tag)::value, NPH = 8 / NQT;
@@ -740,7 +755,7 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
     }
   };
 
-  for_parts<true>(sh, B, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G, Hkv, [&](const Part& un) {
+  for_parts<true>(sh, B, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G, Hkv, s_seq, [&](const Part& un) {
     if (tid == 0) s_bad = 0;
     __syncthreads();                                    // LDS of the unit before is no longer read
     if (un.R > 64) run(std::integral_constant<int, 4>{}, un);
