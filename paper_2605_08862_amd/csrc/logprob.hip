@@ -65,9 +65,9 @@ struct SelectShared {
   Top best[4];
 };
 
-// The n best of the elements that the threads have, E each; -inf and NaN are none.  zmax: the thread's largest.  src.show(p): called by the threads with a
-// candidate, up to kOwners of a wave, puts the thread's elements in place p; src.seen(p, owner, e): element e of the thread `owner` shown in place p; src.own(e):
-// of the calling thread.  out(rank, z, j) is called once for every rank that is taken; returns how many are.
+// The n best of the elements that the threads have, E each; -inf and NaN are none.  zmax: the thread's largest.  src.own(e): element e of the calling thread.  Many
+// elements (Source::kMany): src.show(p), called by the threads with a candidate, up to kOwners of a wave, puts the thread's elements in place p; src.value(p, e):
+// element e of place p, whose thread is `owner`, src.index(owner, e): its token.  out(rank, z, j) is called once for every rank that is taken; returns how many are.
 template <int E, typename Source, typename Out>
 __device__ __forceinline__ int select_top(float zmax, int n, const Source& src, const Out& out, SelectShared& s) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -83,27 +83,59 @@ __device__ __forceinline__ int select_top(float zmax, int n, const Source& src, 
     if (__popcll(__ballot(g >= t)) >= n) key = t;
   }
   const float bound = key <= 0x007fffffu ? -INFINITY : __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
-  // the elements of the few threads that have a candidate, one by each lane
-  for (unsigned long long have = __ballot(zmax >= bound && zmax > -INFINITY); have;) {
-    const int p = __popcll(have & ((1ull << lane) - 1));
-    if ((have >> lane & 1) && p < kOwners) src.show(p);
-    wave_fence();
+  // candidates go to the list a wave at a time
+  auto put = [&](bool hit, unsigned long long hits, int at, float z, int j) {
+    const int k = at + __popcll(hits & ((1ull << lane) - 1));
+    if (hit && k < kList) { s.list[k] = Top{z, j}; s.rank[k] = 0; }
+  };
+  auto reserve = [&](int count) {
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&s.n, count);
+    return __builtin_amdgcn_readfirstlane(at);
+  };
+  auto hit = [&](float z) { return z >= bound && z > -INFINITY; };
+  if constexpr (Source::kMany) {
+    // the elements of the few threads that have one, one by each lane
+    constexpr int C = E / 64;
+    for (unsigned long long have = __ballot(hit(zmax)); have;) {
+      const int p = __popcll(have & ((1ull << lane) - 1));
+      if ((have >> lane & 1) && p < kOwners) src.show(p);
+      wave_fence();
+      float z[kOwners][C];
 #pragma unroll
-    for (int p = 0; p < kOwners; ++p) {
-      if (!have) break;
-      const int owner = wave * 64 + __ffsll((long long)have) - 1;
-      have &= have - 1;
+      for (int o = 0; o < kOwners; ++o)
 #pragma unroll
-      for (int e0 = 0; e0 < E; e0 += 64) {
-        if (e0 + lane >= E) continue;
-        const Top t = src.seen(p, owner, e0 + lane);
-        if (t.z >= bound && t.z > -INFINITY) {
-          const int k = atomicAdd(&s.n, 1);
-          if (k < kList) { s.list[k] = t; s.rank[k] = 0; }
+        for (int c = 0; c < C; ++c) z[o][c] = src.value(o, c * 64 + lane);
+      const int shown = min((int)__popcll(have), kOwners);
+      int count = 0;
+#pragma unroll
+      for (int o = 0; o < kOwners; ++o)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          if (o >= shown) z[o][c] = -INFINITY;           // (what was shown there before)
+          count += __popcll(__ballot(hit(z[o][c])));
+        }
+      int at = reserve(count);
+#pragma unroll
+      for (int o = 0; o < kOwners; ++o) {
+        const int owner = wave * 64 + __ffsll((long long)have) - 1;
+        have &= have - 1;                                // (0 stays 0)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const unsigned long long hits = __ballot(hit(z[o][c]));
+          if (!hits) continue;
+          put(hit(z[o][c]), hits, at, z[o][c], src.index(owner, c * 64 + lane));
+          at += __popcll(hits);
         }
       }
+      wave_fence();
     }
-    wave_fence();
+  } else {
+    for (int e = 0; e * kThreads < src.n; ++e) {
+      const Top t = src.own(e);
+      const unsigned long long hits = __ballot(hit(t.z));
+      if (hits) put(hit(t.z), hits, reserve(__popcll(hits)), t.z, t.j);
+    }
   }
   __syncthreads();
   const int found = s.n;
@@ -112,6 +144,7 @@ __device__ __forceinline__ int select_top(float zmax, int n, const Source& src, 
     for (int k = lane; k < found; k += 64) {
       const Top t = s.list[k];
       int rank = 0;
+#pragma unroll 4
       for (int o = o0; o < o1; ++o) { const Top x = s.list[o]; rank += better(x.z, x.j, t.z, t.j) ? 1 : 0; }
       if (rank) atomicAdd(&s.rank[k], rank);
     }
@@ -146,6 +179,7 @@ __device__ __forceinline__ int select_top(float zmax, int n, const Source& src, 
 
 // A segment: element e of a thread is j0 + (e / P * kThreads + thread) * P + e % P, in vector e / P.
 template <typename T> struct SegmentSource {
+  static constexpr bool kMany = true;
   const u32x4 (&v)[kVecs];
   const T* z0;
   int j0, j1;
@@ -155,9 +189,7 @@ template <typename T> struct SegmentSource {
 #pragma unroll
     for (int u = 0; u < kVecs; ++u) s.stage[threadIdx.x >> 6][p][u] = v[u];
   }
-  __device__ __forceinline__ Top seen(int p, int owner, int e) const {
-    return Top{to_f32<T>(((const T*)s.stage[threadIdx.x >> 6][p])[e]), index(owner, e)};
-  }
+  __device__ __forceinline__ float value(int p, int e) const { return to_f32<T>(((const T*)s.stage[threadIdx.x >> 6][p])[e]); }
   __device__ __forceinline__ Top own(int e) const {
     const int j = index(threadIdx.x, e);
     return Top{j < j1 ? to_f32<T>(z0[j]) : -INFINITY, j};
@@ -165,12 +197,13 @@ template <typename T> struct SegmentSource {
 };
 // The alternatives of a row's segments, in LDS.
 struct PartsSource {
+  static constexpr bool kMany = false;
   int n;
   SelectShared& s;
-  __device__ __forceinline__ Top at(int i) const { return i < n ? s.parts[i] : Top{-INFINITY, 0x7fffffff}; }
-  __device__ __forceinline__ void show(int) const {}
-  __device__ __forceinline__ Top seen(int, int owner, int e) const { return at(e * kThreads + owner); }
-  __device__ __forceinline__ Top own(int e) const { return at(e * kThreads + threadIdx.x); }
+  __device__ __forceinline__ Top own(int e) const {
+    const int i = e * kThreads + threadIdx.x;
+    return i < n ? s.parts[i] : Top{-INFINITY, 0x7fffffff};
+  }
 };
 
 // Maximum and sums of a part of a row, in units of log2: t = (z - m) c with c = log2(e) / T;  s = sum 2^t, q = sum 2^t t.
@@ -214,9 +247,11 @@ __device__ __forceinline__ bool find_row(const LogprobArgs& a, int entry, bool w
   return true;
 }
 
+// 1152 rows of 152064 float32 logits, the 20 best: 142 us, 4.7 TB/s; of bf16 101 us (without alternatives 74).  Registers for five waves on a SIMD: float32 160 us with
+// four; bf16 rows, which have twice the elements, would spill (118 us).
 // seg: elements of a segment, a multiple of 8; segs of them cover a row.  Partials: [entry][segs] statistics, [entry][segs][n_top] alternatives.
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads) logprob_kernel(LogprobArgs a, int seg, int segs, wt_f32x4* __restrict__ part, Top* __restrict__ part_top,
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 4) logprob_kernel(LogprobArgs a, int seg, int segs, wt_f32x4* __restrict__ part, Top* __restrict__ part_top,
                                                            int32_t* __restrict__ counters) {
   __shared__ SelectShared s_sel;
   __shared__ Stats s_stats[4];
@@ -304,8 +339,9 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(LogprobArgs a, int se
         tmax = fmaxf(tmax, p[0]);
       }
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) st = merge_stats(st, Stats{__shfl_xor(st.m, o), __shfl_xor(st.s, o), __shfl_xor(st.q, o)}, c);
+    for (int o = 1; o < segs; o <<= 1) st = merge_stats(st, Stats{__shfl_xor(st.m, o), __shfl_xor(st.s, o), __shfl_xor(st.q, o)}, c);
+    auto first = [](float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); };
+    st = Stats{first(st.m), first(st.s), first(st.q)};
     __syncthreads();
     if constexpr (TOP) {
       n_found = select_top<kMergeEach>(tmax, a.n_top, PartsSource{segs * a.n_top, s_sel}, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
@@ -328,7 +364,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(LogprobArgs a, int se
 }
 
 // Segments of a row: as long as the registers of a workgroup take (kVecs vectors a thread), shorter where there are few rows.  Below kSegLeast words the merge of
-// one more segment costs what its shorter pass saves: 9 rows of 151936 bf16 words in segments of 2048 words 22.7 us, 4096 18.8, 8192 16.4, 16384 16.1; 64 rows of float32 23.0, 22.9,
+// one more segment costs what its shorter pass saves: 9 rows of 151936 bf16 words in segments of 2048 words 22.7 us, 4096 18.8, 8192 16.4, 16384 16.1 (14.4 with a faster merge since); 64 rows of float32 23.0, 22.9,
 // 22.9, 21.3; 500 rows of 8000 26.9, 20.4, 13.4, 13.5.
 struct Cutting { int seg, segs; };
 constexpr int kSegLeast = 16384, kWanted = 1024;
