@@ -70,7 +70,19 @@ struct Shares {
 };
 
 // A sequence that the thread which counted it leaves for the others: the one that this workgroup's share begins in.
-struct Seq { int b, first, end, row0, n, c, slot; };
+struct Seq { int b, n, c, slot; };
+// Sum over the lanes up to this one.
+__device__ __forceinline__ int wave_scan(int v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);            // row_shr 1, 2, 4, 8: in rows of sixteen lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);            // row_bcast 15 to rows 1 and 3, row_bcast 31 to rows 2 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+#endif
+  return v;
+}
 
 // Called by all threads.  s_start, s_row [B + 1]: where every sequence begins, and its first packed row; s_scan: 2 words for each wave; s_seq: see above.
 // A share is no shorter than `least`, and longer than a step, so that every share between two others of a unit has a step of it.
@@ -80,7 +92,7 @@ __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_sl
                                               int32_t* __restrict__ status) {
   constexpr int NW = THREADS / 64, RP = kBlock<WIDE>;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  // few sequences: up to 64 threads share the blocks of one, and the first of them has its place in the prefix sum; many: a thread has a run of them
+  // few sequences: up to 64 threads share the blocks of one; many: a thread has a run of them
   int subs = 1;
   while (subs < 64 && 2 * subs * B <= THREADS) subs *= 2;
   const int per = subs > 1 ? 1 : (B + THREADS - 1) / THREADS, sub = tid & (subs - 1), at = tid / subs;
@@ -98,15 +110,8 @@ __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_sl
     for (int qb = sub; qb * RP < n * G.g; qb += subs) s += 2 * kUnitHalf<WIDE> + step_cost<WIDE>(n * G.g - qb * RP) * block_steps<RP>(c, n, G, qb);
     cost += s * Hkv;
   }
-  for (int o = 1; o < subs; o <<= 1) cost += __shfl_xor(cost, o);
-  if (sub > 0) cost = 0;
   if (fault && blockIdx.x == 0 && status) atomicOr(status, fault);
-  int is = cost, ir = rows;                             // exclusive prefix over the threads
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int a = __shfl_up(is, o), r = __shfl_up(ir, o);
-    if (lane >= o) { is += a; ir += r; }
-  }
+  const int is = wave_scan(cost), ir = wave_scan(rows);
   if (lane == 63) { s_scan[wave] = is; s_scan[NW + wave] = ir; }
   __syncthreads();
   int bs = is - cost, br = ir - rows, total = 0;
@@ -120,18 +125,16 @@ __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_sl
   sh.W = __builtin_amdgcn_readfirstlane(min((int)gridDim.x, max(1, total / least)));
   sh.per = (unsigned long long)((double)sh.total * 65536.0 / (double)sh.W);    // the same in every workgroup; (W - 1) per is below the total
   sh.inv = (float)sh.W / (float)max(sh.total, 1);
-  if (sub == 0) {
-    const int p0 = sh.bound(blockIdx.x);
+  const int p0 = sh.bound(blockIdx.x);
+  const bool mine = bs <= p0 && p0 < bs + cost;
+  if (mine && per == 1) *s_seq = Seq{at, n, c, slot};
+  if (sub == 0)
     for (int b = lo; b < hi; ++b) {
-      const int first = s_start[b] + bs, row0 = s_row[b] + br, end = b + 1 < hi ? s_start[b + 1] + bs : bs + cost;
+      const int first = s_start[b] + bs, end = b + 1 < hi ? s_start[b + 1] + bs : bs + cost;
       s_start[b] = first;
-      s_row[b] = row0;
-      if (first <= p0 && p0 < end) {
-        if (per > 1) { n = seq_n[b] + n_add; slot = seq_slot[b]; c = seq_pos[b]; }
-        *s_seq = Seq{b, first, end, row0, n, c, slot};
-      }
+      s_row[b] += br;
+      if (mine && per > 1 && first <= p0 && p0 < end) *s_seq = Seq{b, seq_n[b] + n_add, seq_pos[b], seq_slot[b]};
     }
-  }
   if (tid == 0) s_start[B] = total;
   __syncthreads();
   return sh;
@@ -172,14 +175,14 @@ __device__ __forceinline__ void enter_sequence(Unit<WIDE>& u, const int* s_start
 }
 // The unit that p lies in, of the sequence that p lies in.
 template <bool WIDE>
-__device__ __forceinline__ Unit<WIDE> unit_at(int p, const Seq& s, Group G, int Hkv) {
+__device__ __forceinline__ Unit<WIDE> unit_at(int p, const Seq& s, const int* s_start, const int* s_row, Group G, int Hkv) {
   Unit<WIDE> u;
   auto same = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
-  u.b = same(s.b); u.n = same(s.n); u.c = same(s.c); u.slot = same(s.slot); u.row0 = same(s.row0); u.first = same(s.first);
+  u.b = same(s.b); u.n = same(s.n); u.c = same(s.c); u.slot = same(s.slot); u.row0 = same(s_row[u.b]); u.first = same(s_start[u.b]);
   u.blocks = (u.n * G.g + kBlock<WIDE> - 1) / kBlock<WIDE>;
   u.h = u.qb = 0;
   fill_unit<WIDE>(u, G);
-  const int head = u.blocks == 1 ? u.end() - u.first : (same(s.end) - u.first) / Hkv;
+  const int head = u.blocks == 1 ? u.end() - u.first : (same(s_start[u.b + 1]) - u.first) / Hkv;
   int h = min(Hkv - 1, (int)((float)(p - u.first) / (float)head));
   while (h > 0 && h * head > p - u.first) --h;
   while (h + 1 < Hkv && (h + 1) * head <= p - u.first) ++h;
@@ -231,7 +234,7 @@ __device__ __forceinline__ void for_parts(const Shares& sh, int B, const int* s_
   const int w = blockIdx.x;
   if (w >= sh.W || sh.total == 0) return;
   const int p0 = __builtin_amdgcn_readfirstlane(sh.bound(w)), p1 = __builtin_amdgcn_readfirstlane(sh.bound(w + 1));
-  Unit<WIDE> u = unit_at<WIDE>(p0, s_seq, G, Hkv);
+  Unit<WIDE> u = unit_at<WIDE>(p0, s_seq, s_start, s_row, G, Hkv);
   int s_lo = u.cut(p0);
   while (true) {
     const bool last = u.end() >= p1;
