@@ -239,10 +239,11 @@ __device__ __forceinline__ void for_parts(const Shares& sh, int B, const int* s_
   while (true) {
     const bool last = u.end() >= p1;
     const int s_hi = last ? u.cut(p1) : u.steps;
-    const Unit<WIDE> now = u;
+    const bool any = s_lo < s_hi;
+    const Part part = part_of<WIDE>(u, sh, s_lo, s_hi, G);
     // the next unit is looked up in front of this one's work, which covers the trip to memory
     const bool more = !last && next_unit<WIDE>(u, B, Hkv, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G);
-    if (s_lo < s_hi) f(part_of<WIDE>(now, sh, s_lo, s_hi, G));
+    if (any) f(part);
     s_lo = 0;
     if (!more) break;
   }
