@@ -78,7 +78,7 @@ __device__ __forceinline__ float bounded(float f) { return f != f ? 0.f : fminf(
 // One workgroup per (page of a sequence, KV head): two waves have K, two V.  All of a thread's rows are loaded before the scale is known and stay in registers.
 // K: a thread has sixteen d of a token, which are sixteen bytes of the page; V: four d of sixteen tokens, transposed in registers into four times sixteen bytes.
 // No two threads write the same sixteen bytes, so older rows that have to be rounded again need no barrier.  Many rows: bound by memory, 32016 rows x 4 heads x 128
-// (16 prompts of the 7B heads) 25 us, 3.9 TB/s of rows and codes.  A row each of 64 sequences: 6 us, a chain of trips to memory (the batch's numbers, the
+// (16 prompts of the 7B heads) written and read back 53 us, 3.7 TB/s of rows and codes.  A row each of 64 sequences: 6 us, a chain of trips to memory (the batch's numbers, the
 // page's id, its scale and the row) and the launch.
 template <Source S, int D>
 __global__ void __launch_bounds__(256) kvq_write_kernel(KvqView kv, KvqSeqs q, int pages_each, const void* __restrict__ k_rows, const void* __restrict__ v_rows,
@@ -87,8 +87,9 @@ __global__ void __launch_bounds__(256) kvq_write_kernel(KvqView kv, KvqSeqs q, i
   __shared__ int s_red[8];
   __shared__ uint32_t s_max[4];
   constexpr int PK = D / 32, KD = D / 16, VD = D / 4;   // K pieces of a thread, of a row; threads for the d of V
-  const int b = blockIdx.x / pages_each, h = blockIdx.y, is_v = __builtin_amdgcn_readfirstlane(threadIdx.x >> 7), t = threadIdx.x & 127;
-  const Span sp = find_span<true>(kv, q, b, blockIdx.x % pages_each, s_red, blockIdx.y == 0 ? status : nullptr);
+  const int nth = (int)(blockIdx.z * gridDim.y + blockIdx.y), b = nth / pages_each, h = blockIdx.x, is_v = __builtin_amdgcn_readfirstlane(threadIdx.x >> 7), t = threadIdx.x & 127;
+  if (b >= q.B) return;
+  const Span sp = find_span<true>(kv, q, b, nth - b * pages_each, s_red, h == 0 ? status : nullptr);
   if (!sp.live) return;
   const T* rows = (const T*)(is_v ? v_rows : k_rows);
   uint8_t* page = (is_v ? kv.v : kv.k) + (size_t)sp.page * kvq_page_bytes(kv.Hkv, D);
@@ -250,14 +251,15 @@ __global__ void __launch_bounds__(256) kvq_write_kernel(KvqView kv, KvqSeqs q, i
 
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) { return __float_as_uint(a) >> 16 | (__float_as_uint(b) & 0xffff0000u); }   // exact: four significant bits
 
-// As kvq_write_kernel, the other way: the same rows 20 us, the same 64 rows 6 us.
+// As kvq_write_kernel, the other way.
 template <bool VEC, int D>
 __global__ void __launch_bounds__(256) kvq_read_kernel(KvqView kv, KvqSeqs q, int pages_each, bf16* __restrict__ k_rows, bf16* __restrict__ v_rows,
                                                        size_t stride, int32_t* __restrict__ status) {
   __shared__ int s_red[8];
   constexpr int PK = D / 32, KD = D / 16, VD = D / 4;
-  const int b = blockIdx.x / pages_each, h = blockIdx.y, is_v = __builtin_amdgcn_readfirstlane(threadIdx.x >> 7), t = threadIdx.x & 127;
-  const Span sp = find_span<false>(kv, q, b, blockIdx.x % pages_each, s_red, blockIdx.y == 0 ? status : nullptr);
+  const int nth = (int)(blockIdx.z * gridDim.y + blockIdx.y), b = nth / pages_each, h = blockIdx.x, is_v = __builtin_amdgcn_readfirstlane(threadIdx.x >> 7), t = threadIdx.x & 127;
+  if (b >= q.B) return;
+  const Span sp = find_span<false>(kv, q, b, nth - b * pages_each, s_red, h == 0 ? status : nullptr);
   if (!sp.live) return;
   const uint8_t* page = (is_v ? kv.v : kv.k) + (size_t)sp.page * kvq_page_bytes(kv.Hkv, D);
   const float f = kvq_scale(kvq_exp_of((is_v ? kv.vs : kv.ks)[(size_t)sp.page * kv.Hkv + h]));
@@ -313,10 +315,15 @@ __global__ void __launch_bounds__(256) kvq_read_kernel(KvqView kv, KvqSeqs q, in
 }
 
 int pages_each(const KvqSeqs& q) { return (q.n_max + 2 * kPage - 2) / kPage; }   // pages that n_max rows touch at most
+// The heads of a page side by side: their rows are neighbours in memory (16 prompts 53 us, with the heads far apart 58).
+dim3 grid_of(const KvqView& kv, const KvqSeqs& q) {
+  const long long pages = (long long)q.B * pages_each(q), z = (pages + 65534) / 65535;
+  return dim3(kv.Hkv, (unsigned)((pages + z - 1) / z), (unsigned)z);
+}
 }  // namespace
 
 void launch_kvq_write(const KvqView& kv, const KvqSeqs& q, const void* k_rows, const void* v_rows, size_t stride, int32_t* status, hipStream_t st) {
-  const dim3 grid(q.B * pages_each(q), kv.Hkv);
+  const dim3 grid = grid_of(kv, q);
   const bool vec = (((uintptr_t)k_rows | (uintptr_t)v_rows) & 15) == 0 && stride % 8 == 0;
 #define BS_KVQ(S_, D_) hipLaunchKernelGGL((kvq_write_kernel<S_, D_>), grid, dim3(256), 0, st, kv, q, pages_each(q), k_rows, v_rows, stride, status)
   if (kv.D == 128) { if (vec) BS_KVQ(ROWS_VEC, 128); else BS_KVQ(ROWS, 128); }
@@ -324,12 +331,12 @@ void launch_kvq_write(const KvqView& kv, const KvqSeqs& q, const void* k_rows, c
 #undef BS_KVQ
 }
 void launch_kvq_write_staged(const KvqView& kv, const KvqSeqs& q, const void* k_pages, const void* v_pages, int32_t* status, hipStream_t st) {
-  const dim3 grid(q.B * pages_each(q), kv.Hkv);
+  const dim3 grid = grid_of(kv, q);
   if (kv.D == 128) hipLaunchKernelGGL((kvq_write_kernel<STAGED, 128>), grid, dim3(256), 0, st, kv, q, pages_each(q), k_pages, v_pages, (size_t)0, status);
   else hipLaunchKernelGGL((kvq_write_kernel<STAGED, 64>), grid, dim3(256), 0, st, kv, q, pages_each(q), k_pages, v_pages, (size_t)0, status);
 }
 void launch_kvq_read(const KvqView& kv, const KvqSeqs& q, void* k_rows, void* v_rows, size_t stride, int32_t* status, hipStream_t st) {
-  const dim3 grid(q.B * pages_each(q), kv.Hkv);
+  const dim3 grid = grid_of(kv, q);
   const bool vec = (((uintptr_t)k_rows | (uintptr_t)v_rows) & 15) == 0 && stride % 8 == 0;
 #define BS_KVQ(V_, D_) hipLaunchKernelGGL((kvq_read_kernel<V_, D_>), grid, dim3(256), 0, st, kv, q, pages_each(q), (bf16*)k_rows, (bf16*)v_rows, stride, status)
   if (kv.D == 128) { if (vec) BS_KVQ(true, 128); else BS_KVQ(false, 128); }
