@@ -11,12 +11,13 @@
 
 namespace {
 
-constexpr int kThreads = 256, kVecs = 16, kList = 512;  // vectors of sixteen bytes of a thread; places of the list of candidates
-constexpr int kMaxSegs = kLogprobMaxVocab / (kThreads * 64);   // (a lane for each in the merge: at most 64)
+constexpr int kThreads = 256, kEach = 64, kList = 512;  // elements of a thread; places of the list of candidates
+constexpr int kSegment = kThreads * kEach, kMaxSegs = kLogprobMaxVocab / kSegment;       // (a lane for each in the merge: at most 64)
 constexpr int kMergeEach = kMaxSegs * kLogprobMaxTop / kThreads;     // list entries of a thread in the merge
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-template <typename T> constexpr int kPer = 16 / sizeof(T);                    // elements of a vector
+template <typename T> constexpr int kPer = 16 / sizeof(T);                    // elements of a vector of sixteen bytes
+template <typename T> constexpr int kVecs = kEach / kPer<T>;                 // vectors of a thread
 template <typename T> struct Vec;                                            // a vector that starts on any element
 template <> struct Vec<float> { typedef uint32_t V __attribute__((ext_vector_type(4), aligned(4))); };
 template <> struct Vec<bf16> { typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2))); };
@@ -55,15 +56,17 @@ __device__ __forceinline__ bool better(float za, int ja, float zb, int jb) { ret
 constexpr int kOwners = 4;                              // threads of a wave whose elements are looked at together
 struct SelectShared {
   float group[4][64];
-  union {
-    u32x4 stage[4][kOwners][kVecs];                     // elements of those threads
-    Top parts[kMaxSegs * kLogprobMaxTop];               // merge: the segments' alternatives
-  };
   Top list[kList];
   int rank[kList];
   int n;
   Top best[4];
 };
+// Behind it, one after the other: elements of those threads, [wave][kOwners][vector]; in the merge, the segments' alternatives.
+constexpr size_t kStageBytes = (size_t)4 * kOwners * kEach * sizeof(float);
+size_t select_bytes(int segs, int n_top) {
+  const size_t parts = segs > 1 ? (size_t)segs * n_top * sizeof(Top) : 0;
+  return n_top == 0 ? 0 : parts > kStageBytes ? parts : kStageBytes;
+}
 
 // The n best of the elements that the threads have, E each; -inf and NaN are none.  zmax: the thread's largest.  src.own(e): element e of the calling thread.  Many
 // elements (Source::kMany): src.show(p), called by the threads with a candidate, up to kOwners of a wave, puts the thread's elements in place p; src.value(p, e):
@@ -180,16 +183,16 @@ __device__ __forceinline__ int select_top(float zmax, int n, const Source& src, 
 // A segment: element e of a thread is j0 + (e / P * kThreads + thread) * P + e % P, in vector e / P.
 template <typename T> struct SegmentSource {
   static constexpr bool kMany = true;
-  const u32x4 (&v)[kVecs];
+  const u32x4 (&v)[kVecs<T>];
   const T* z0;
   int j0, j1;
-  SelectShared& s;
+  u32x4* stage;                                        // the wave's
   __device__ __forceinline__ int index(int thread, int e) const { return j0 + (e / kPer<T> * kThreads + thread) * kPer<T> + e % kPer<T>; }
   __device__ __forceinline__ void show(int p) const {
 #pragma unroll
-    for (int u = 0; u < kVecs; ++u) s.stage[threadIdx.x >> 6][p][u] = v[u];
+    for (int u = 0; u < kVecs<T>; ++u) stage[p * (kEach / 4) + u] = v[u];
   }
-  __device__ __forceinline__ float value(int p, int e) const { return to_f32<T>(((const T*)s.stage[threadIdx.x >> 6][p])[e]); }
+  __device__ __forceinline__ float value(int p, int e) const { return to_f32<T>(((const T*)(stage + p * (kEach / 4)))[e]); }
   __device__ __forceinline__ Top own(int e) const {
     const int j = index(threadIdx.x, e);
     return Top{j < j1 ? to_f32<T>(z0[j]) : -INFINITY, j};
@@ -199,10 +202,10 @@ template <typename T> struct SegmentSource {
 struct PartsSource {
   static constexpr bool kMany = false;
   int n;
-  SelectShared& s;
+  const Top* parts;
   __device__ __forceinline__ Top own(int e) const {
     const int i = e * kThreads + threadIdx.x;
-    return i < n ? s.parts[i] : Top{-INFINITY, 0x7fffffff};
+    return i < n ? parts[i] : Top{-INFINITY, 0x7fffffff};
   }
 };
 
@@ -247,17 +250,18 @@ __device__ __forceinline__ bool find_row(const LogprobArgs& a, int entry, bool w
   return true;
 }
 
-// 1152 rows of 152064 float32 logits, the 20 best: 142 us, 4.7 TB/s; of bf16 101 us (without alternatives 74).  Registers for five waves on a SIMD: float32 160 us with
-// four; bf16 rows, which have twice the elements, would spill (118 us).
+// 1152 rows of 152064 float32 logits, the 20 best: 142 us, 4.7 TB/s (without alternatives the same rate); of bf16 104 us, where the workgroups' chains of selection bound
+// it (78 without alternatives).  Registers for five waves on a SIMD: float32 160 us with four; for eight: bf16 108 us with seven.
 // seg: elements of a segment, a multiple of 8; segs of them cover a row.  Partials: [entry][segs] statistics, [entry][segs][n_top] alternatives.
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 4) logprob_kernel(LogprobArgs a, int seg, int segs, wt_f32x4* __restrict__ part, Top* __restrict__ part_top,
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 8) logprob_kernel(LogprobArgs a, int seg, int segs, wt_f32x4* __restrict__ part, Top* __restrict__ part_top,
                                                            int32_t* __restrict__ counters) {
+  extern __shared__ __align__(16) char s_more[];
   __shared__ SelectShared s_sel;
   __shared__ Stats s_stats[4];
   __shared__ Top s_top[kLogprobMaxTop];
   __shared__ int s_i[4], s_flag;
-  constexpr int P = kPer<T>, E = kVecs * P;             // elements of a vector, of a thread
+  constexpr int P = kPer<T>;                            // elements of a vector
   const int entry = blockIdx.x / segs, sg = blockIdx.x - entry * segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.vocab;
   size_t row;
   int tok;
@@ -267,10 +271,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 4) logprob_kern
   const float z_tok = to_f32<T>(z0[tok]);
 
   // ---- the segment: element e of a thread is j0 + (e / P * kThreads + tid) * P + e % P
-  u32x4 v[kVecs];
+  u32x4 v[kVecs<T>];
   const uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;           // -inf
 #pragma unroll
-  for (int u = 0; u < kVecs; ++u) {
+  for (int u = 0; u < kVecs<T>; ++u) {
     const int j = j0 + (u * kThreads + tid) * P;
     v[u] = u32x4{none, none, none, none};
     if (j0 + u * kThreads * P >= j1) continue;          // the same for all threads
@@ -287,18 +291,18 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 4) logprob_kern
   }
   float zmax = -INFINITY;                               // (of NaN alone: no maximum)
 #pragma unroll
-  for (int u = 0; u < kVecs; ++u)
+  for (int u = 0; u < kVecs<T>; ++u)
 #pragma unroll
     for (int e = 0; e < P; ++e) zmax = fmaxf(zmax, element<T>(v[u], e));
   const float m = wave_max(zmax);
   if constexpr (P == 8) {                               // unpacked again below: kept, the elements would take 128 registers
 #pragma unroll
-    for (int u = 0; u < kVecs; ++u) asm volatile("" : "+v"(v[u]));
+    for (int u = 0; u < kVecs<T>; ++u) asm volatile("" : "+v"(v[u]));
   }
   const float c = a.inv_temp * 1.44269504088896341f, m0 = m == -INFINITY ? 0.f : m;
   float sum = 0.f, q = 0.f;
 #pragma unroll
-  for (int u = 0; u < kVecs; ++u) {
+  for (int u = 0; u < kVecs<T>; ++u) {
     if (j0 + u * kThreads * P >= j1) break;
 #pragma unroll
     for (int e = 0; e < P; ++e) {
@@ -312,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 4) logprob_kern
   if (lane == 0) s_stats[wave] = Stats{m, sum, q};
   int n_found = 0;
   if constexpr (TOP)
-    n_found = select_top<E>(zmax, a.n_top, SegmentSource<T>{v, z0, j0, j1, s_sel}, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
+    n_found = select_top<kEach>(zmax, a.n_top, SegmentSource<T>{v, z0, j0, j1, (u32x4*)s_more + wave * (kOwners * kEach / 4)}, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
   __syncthreads();
   Stats st = s_stats[0];
 #pragma unroll
@@ -335,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 4) logprob_kern
       const int n = segs * a.n_top;
       for (int i = tid; i < n; i += kThreads) {
         const wt_f32x2 p = wt_load2(bt, i * 8);
-        s_sel.parts[i] = Top{p[0], __float_as_int(p[1])};
+        ((Top*)s_more)[i] = Top{p[0], __float_as_int(p[1])};
         tmax = fmaxf(tmax, p[0]);
       }
     }
@@ -344,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 4) logprob_kern
     st = Stats{first(st.m), first(st.s), first(st.q)};
     __syncthreads();
     if constexpr (TOP) {
-      n_found = select_top<kMergeEach>(tmax, a.n_top, PartsSource{segs * a.n_top, s_sel}, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
+      n_found = select_top<kMergeEach>(tmax, a.n_top, PartsSource{segs * a.n_top, (const Top*)s_more}, [&](int r, float x, int j) { s_top[r] = Top{x, j}; }, s_sel);
       __syncthreads();
     }
   }
@@ -363,35 +367,29 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 4) logprob_kern
     }
 }
 
-// Segments of a row: as long as the registers of a workgroup take (kVecs vectors a thread), shorter where there are few rows.  Below kSegLeast words the merge of
-// one more segment costs what its shorter pass saves: 9 rows of 151936 bf16 words in segments of 2048 words 22.7 us, 4096 18.8, 8192 16.4, 16384 16.1 (14.4 with a faster merge since); 64 rows of float32 23.0, 22.9,
-// 22.9, 21.3; 500 rows of 8000 26.9, 20.4, 13.4, 13.5.
+// Segments of a row: as few as fit (64 elements of a thread in registers), of the same length.  More of them for few rows: the merge of one more costs what its
+// shorter pass saves (9 rows of 151936 bf16 words in segments of 2048 words 22.7 us, 4096 18.8, 8192 16.4, 16384 16.1; 64 rows of float32 23.0, 22.9, 22.9, 21.3; 500
+// rows of 8000 26.9, 20.4, 13.4, 13.5).  Segments of twice the length for bf16: 1152 rows 101 us, with the 20 best,
+// instead of 104, but 64 rows 19.6 instead of 17.8 and 9 rows 14.3 instead of 13.6.
 struct Cutting { int seg, segs; };
-constexpr int kSegLeast = 16384, kWanted = 1024;
-Cutting cut_rows(long long rows, int vocab, int per) {
-  const int longest = kThreads * kVecs * per, least = (vocab + longest - 1) / longest, most = (vocab + kSegLeast - 1) / kSegLeast;
-  const long long want = (kWanted + rows - 1) / rows;
-  int segs = want < least ? least : want > most ? most : (int)want;
-  if (segs > kMaxSegs) segs = kMaxSegs;                 // (never fewer than `least`: kLogprobMaxVocab)
-  const int seg = ((vocab + segs - 1) / segs + 7) / 8 * 8;
-  return Cutting{seg, (vocab + seg - 1) / seg};
+Cutting cut_rows(int vocab) {
+  const int segs = (vocab + kSegment - 1) / kSegment;
+  return Cutting{((vocab + segs - 1) / segs + 7) / 8 * 8, segs};
 }
 }  // namespace
 
 size_t logprob_workspace(int B, int k_max, int vocab, int n_top) {
-  const long long rows = (long long)B * (k_max + 1), least = (vocab + kThreads * kVecs * kPer<float> - 1) / (kThreads * kVecs * kPer<float>);
-  const long long parts = rows * least > kWanted + rows ? rows * least : kWanted + rows;   // of this many rows or of fewer
-  return (size_t)kLogprobMaxRows * sizeof(int32_t) + parts * (sizeof(wt_f32x4) + (size_t)n_top * sizeof(Top)) + 256;
+  return (size_t)kLogprobMaxRows * sizeof(int32_t) + (size_t)B * (k_max + 1) * cut_rows(vocab).segs * (sizeof(wt_f32x4) + (size_t)n_top * sizeof(Top));
 }
 
 void launch_logprob(const LogprobArgs& a, int B, int dtype, void* workspace, hipStream_t st) {
   const long long rows = (long long)B * (a.k_max + 1);
-  const Cutting cut = cut_rows(rows, a.vocab, dtype == BS_F32 ? kPer<float> : kPer<bf16>);
+  const Cutting cut = cut_rows(a.vocab);
   int32_t* counters = (int32_t*)workspace;
   wt_f32x4* part = (wt_f32x4*)(counters + kLogprobMaxRows);
   Top* part_top = (Top*)(part + rows * cut.segs);
   const dim3 grid((unsigned)(rows * cut.segs));
-#define BS_LOGPROB(T_, TOP_) hipLaunchKernelGGL((logprob_kernel<T_, TOP_>), grid, dim3(kThreads), 0, st, a, cut.seg, cut.segs, part, part_top, counters)
+#define BS_LOGPROB(T_, TOP_) hipLaunchKernelGGL((logprob_kernel<T_, TOP_>), grid, dim3(kThreads), select_bytes(cut.segs, a.n_top), st, a, cut.seg, cut.segs, part, part_top, counters)
   if (dtype == BS_F32) { if (a.n_top > 0) BS_LOGPROB(float, true); else BS_LOGPROB(float, false); }
   else { if (a.n_top > 0) BS_LOGPROB(bf16, true); else BS_LOGPROB(bf16, false); }
 #undef BS_LOGPROB
