@@ -250,7 +250,7 @@ __device__ __forceinline__ bool find_row(const LogprobArgs& a, int entry, bool w
   return true;
 }
 
-// 1152 rows of 152064 float32 logits, the 20 best: 142 us, 4.7 TB/s (without alternatives the same rate); of bf16 104 us, where the workgroups' chains of selection bound
+// 1152 rows of 152064 float32 logits, the 20 best: 142 us, 4.7 TB/s (130 without alternatives); of bf16 104 us, where the workgroups' chains of selection bound
 // it (78 without alternatives).  Registers for five waves on a SIMD: float32 160 us with four; for eight: bf16 108 us with seven.
 // seg: elements of a segment, a multiple of 8; segs of them cover a row.  Partials: [entry][segs] statistics, [entry][segs][n_top] alternatives.
 template <typename T, bool TOP>
