@@ -1,12 +1,16 @@
 """CPU-only: what bs_kvq_* and bs_token_logprobs refuse on the host, before anything is launched.  The pointers are made up; a call that
-passes every check ends in BS_EHIP here, where no GPU is."""
+passes every check ends in BS_EHIP here, where no GPU is.  And what the compiled kernels hold in registers and wait for."""
 import ctypes as C
 import os
+import re
+import shutil
+import subprocess
 
 import pytest
 import torch
 
 from paper_2605_08862_amd import binding as B
+from paper_2605_08862_amd import build as BLD
 
 P = 1 << 20          # an aligned address that nothing is read from
 
@@ -88,3 +92,44 @@ def test_logprobs(lib):
     assert call(z=P + 2, dtype=B.BS_BF16) == B.BS_EHIP
     for bad in [(0, 4, 1000, 5), (3, -1, 1000, 5), (3, 4, 1, 0), (3, 4, 1000, 33), (3, 4, 3, 4), (4096, 300, 1000, 5)]:
         assert B.bs_token_logprobs_workspace_bytes(*bad) == 0, bad
+
+
+@pytest.fixture(scope="module")
+def assembly(tmp_path_factory):
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    if not (os.path.exists(hipcc) or shutil.which(hipcc)):
+        pytest.skip("hipcc not available")
+    out = {}
+    for name in ("kvq_attention", "logprob", "kvq"):
+        path = tmp_path_factory.mktemp("asm") / (name + ".s")
+        r = subprocess.run([hipcc, *BLD.FLAGS, "--offload-device-only", "-S", os.path.join(BLD.CSRC, name + ".hip"), "-o", str(path)], capture_output=True, text=True)
+        assert r.returncode == 0, r.stderr[-2000:]
+        out[name] = path.read_text()
+    return out
+
+
+def test_no_kernel_spills(assembly):
+    """The accumulators, tiles and rows that the kernels keep in registers stay there."""
+    spills = {n: int(s) for text in assembly.values() for n, s in re.findall(r"\.symbol:\s+(\S+)\.kd.*?\.vgpr_spill_count:\s+(\d+)", text, re.S)}
+    assert len(spills) >= 18 and not any(spills.values()), spills
+
+
+def test_requests_of_the_shared_tiles_are_counted_right(assembly):
+    """The attention kernel for many rows waits for all but the N newest of its requests to memory, N a multiple of those of a tile: its loops hold these requests,
+    and nothing else that counts."""
+    loops = []
+    for name, body in re.findall(r"^(\S*kvq_wide_kernelILi\d+\S*):[^\n]*\n(.*?)s_endpgm", assembly["kvq_attention"], re.S | re.M):
+        D = int(re.search(r"ILi(\d+)", name)[1])
+        for wait in re.finditer(r"s_waitcnt vmcnt\(([1-9]\d*)\) lgkmcnt\(0\)\n\ts_barrier", body):
+            inside = []                                                       # backward branches over the wait: the innermost is its loop's
+            for b in re.finditer(r"s_c?branch\S* (\.LBB\d+_\d+)", body[wait.start():]):
+                end, start = wait.start() + b.end(), body.index("\n" + b[1] + ":")
+                if start < wait.start():
+                    inside.append((end - start, start, end))
+            _, start, end = min(inside)
+            ops = re.findall(r"^\t((?:global|buffer|flat|scratch)_\S+)", body[start:end], re.M)
+            loops.append((D, int(wait[1]), sorted(ops)))
+    expected = {(128, 5): 4, (128, 12): 2, (64, 3): 2, (64, 8): 1}         # (head size, N): sixteen-byte requests of a tile; and one for the scales
+    assert len(loops) == 8
+    for D, n, ops in loops:
+        assert ops == ["global_load_lds_dword"] + ["global_load_lds_dwordx4"] * expected[D, n], (D, n, ops)
