@@ -409,3 +409,22 @@ def test_batches_without_rows_and_repeated_slots():
     a, _ = x.cache.read(0, _i32([s, s, s]), _i32([10, 0, 64]), _i32([100, 110, 3]), 110, 213)
     b, _ = x.cache.read(0, _i32([s]), _i32([0]), _i32([110]), 110, 110)
     assert torch.equal(a[:100], b[10:]) and torch.equal(a[100:210], b) and torch.equal(a[210:], b[64:67]) and x.cache.poll_status() == 0
+
+
+def test_pages_behind_four_gib():
+    """A pool of 4.3 GiB for K and as much for V: what is held and attended in its last pages is what a small cache gives."""
+    H, D, n, far = 8, 128, 600, 70000
+    big = KvqCache(1, H, H, D, 2, 0, 40, device=DEV, slot_tokens=[far * 64, n])
+    small = KvqCache(1, H, H, D, 2, 0, 40, device=DEV, slot_tokens=[64, n])
+    g = torch.Generator(device=DEV).manual_seed(5)
+    k, v, q = (torch.randn(m, H, D, generator=g, device=DEV).to(torch.bfloat16) for m in (n, n, 240))
+    assert int(big.block_table[1, 0]) == far
+    for c in (big, small):
+        c.write(0, _i32([1]), _i32([0]), _i32([n]), n, k, v)
+    for a, b in zip(big.read(0, _i32([1]), _i32([0]), _i32([n]), n, n), small.read(0, _i32([1]), _i32([0]), _i32([n]), n, n)):
+        assert torch.equal(a, b)
+    for slots, rows in (([1], 1), ([1], 40), ([1] * 6, 40)):                # few rows, blocks of them, and the kernel for many
+        args = _i32(slots), _i32([n - rows] * len(slots)), _i32([rows] * len(slots)), rows
+        got, want = (c.attention(0, q[:rows * len(slots)], *args).double() for c in (big, small))
+        assert bool((got - want).abs().max() <= 2.0 ** -6 * want.abs().max()), (len(slots), rows)
+    assert big.poll_status() == 0 and small.poll_status() == 0
