@@ -733,22 +733,23 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
           *(f32x4*)(mine + ln * LDO + d2 * 32 + 8 * i4 + 4 * lg) = f32x4{a[4 * i4], a[4 * i4 + 1], a[4 * i4 + 2], a[4 * i4 + 3]};
         }
       __syncthreads();
-      for (int it = tid; it < un.R * (CH / 2); it += 512) {
-        const int r = it / (CH / 2), ch = it % (CH / 2), tq = r / 32, lr = r % 32;
+#pragma unroll
+      for (int j = 0; j < NQT * 32 * (CH / 2) / 512; ++j) {                 // all rows of the query tiles, so that the loads are in flight together
+        const int it = tid + 512 * j, r = it / (CH / 2), ch = it % (CH / 2), tq = r / 32, lr = r % 32;
         float mw[NPH], mt = -INFINITY, lt = 0.f;
 #pragma unroll
         for (int w = 0; w < NPH; ++w) { mw[w] = s_m[(tq * NPH + w) * 32 + lr]; mt = fmaxf(mt, mw[w]); }
         f32x4 acc{0.f, 0.f, 0.f, 0.f};
-        if (mt != -INFINITY)
 #pragma unroll
-          for (int w = 0; w < NPH; ++w) {
-            const float f = __builtin_amdgcn_exp2f(mw[w] - mt);
-            lt += s_l[(tq * NPH + w) * 32 + lr] * f;
-            const f32x4 v = *(const f32x4*)(s_o + ((size_t)(tq * NPH + w) * 32 + lr) * LDO + ch * 4);
+        for (int w = 0; w < NPH; ++w) {
+          const float f = mw[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[w] - mt);
+          lt += s_l[(tq * NPH + w) * 32 + lr] * f;
+          const f32x4 v = *(const f32x4*)(s_o + ((size_t)(tq * NPH + w) * 32 + lr) * LDO + ch * 4);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] += v[e] * f;
-          }
+          for (int e = 0; e < 4; ++e) acc[e] += v[e] * f;
+        }
         const int col = half * DH + ch * 4;
+        if (r >= un.R) continue;
         if (!un.whole) {
           wt_store4(bo, ((part + r) * D + col) * 4, acc);
           if (half == 0 && ch == 0) wt_store2(bm, (part + r) * 8, bad_unit ? INFINITY : mt, lt);
