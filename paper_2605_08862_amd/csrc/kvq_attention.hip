@@ -40,11 +40,12 @@ __device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
 // All units in a row (sequence, KV head, block) have a length: kUnitHalf, step_cost for each of their steps, kUnitHalf, in units of 1/8 step of a launch that is bound
 // by memory.  The workgroups cut that into W equal parts; a cut is moved to the next step's start, and to the unit's end or start where less than kSnap + 1
 // steps would be left on that side.  So a share is a run of steps, and what a unit costs besides its steps (its queries, the merge of the waves) counts.
-// Measured around the values (us; 128 sequences of 100 .. 16000 tokens, 1 .. 17 rows, and 100 of 3000 tokens, 17 rows; 7B heads): kUnitHalf of the wide kernel 24, 40,
-// 56: 229, 222, 226 and 130, 127, 130; its step_cost of more than 64 rows 10, 12, 14: 261, 222, 234 and 128, 127, 131.
+// Measured in the wide kernel, 128 sequences of 1 .. 17 rows and 500 .. 32000 tokens, 7B heads: a step of up to 32, 64 and more rows 0.97, 1.25 and 2.27 us, a unit
+// besides its steps 10 us.  With 12 for the last, and 8 for both others, this batch took 227 us and 100 sequences around 3000 tokens 114; with 14 211 and 107, with 15 209
+// and 103; kUnitHalf 24, 28, 32, 36: 211, 210, 209, 211 and 106, 104, 103, 105.
 constexpr int kSnap = 2;
-template <bool WIDE> constexpr int kUnitHalf = WIDE ? 36 : 8;             // on either side of a unit's steps
-template <bool WIDE> __device__ __forceinline__ int step_cost(int R) { return !WIDE ? 8 : R > 64 ? 14 : R > 32 ? 8 : 6; }
+template <bool WIDE> constexpr int kUnitHalf = WIDE ? 32 : 8;             // on either side of a unit's steps
+template <bool WIDE> __device__ __forceinline__ int step_cost(int R) { return !WIDE ? 8 : R > 64 ? 15 : R > 32 ? 8 : 6; }
 template <bool WIDE> constexpr int kBlock = WIDE ? 128 : 32;          // rows of a block
 // Query heads of a KV head.  x / g by a product with 2^32 / g rounded up: exact for x below 2^32 / g, i.e. any packed row.
 struct Group {
@@ -148,7 +149,7 @@ struct Unit {
   __device__ __forceinline__ int end() const { return first + 2 * kUnitHalf<WIDE> + step * steps; }
   // step at which a cut at p is made
   __device__ __forceinline__ int cut(int p) const {
-    const int x = max(p - first - kUnitHalf<WIDE>, 0) + step - 1, j = (int)__umulhi((uint32_t)x, step == 8 ? 536870912u : step == 14 ? 306783379u : 715827883u);   // / step
+    const int x = max(p - first - kUnitHalf<WIDE>, 0) + step - 1, j = (int)__umulhi((uint32_t)x, step == 8 ? 536870912u : step == 15 ? 286331154u : 715827883u);   // / step
     return p >= end() ? steps : p <= first + kUnitHalf<WIDE> + kSnap * step ? 0 : steps - j <= kSnap ? steps : j;
   }
   // the first and the last workgroup that have steps of the unit
@@ -795,7 +796,7 @@ void launch(const KvqView& kv, const KvqSeqs& s, int Hq, const void* q, size_t q
   const bool wide = runs_wide(kv, s, Hq / kv.Hkv);
   const int RP = wide ? 128 : 32, G = Hq / kv.Hkv, least = 32;
   // no more workgroups than shares, of sequences as long as the block table is wide
-  const long long blocks = ((long long)s.n_max * G + RP - 1) / RP, most = (long long)s.B * kv.Hkv * blocks * (2 * (wide ? kUnitHalf<true> : kUnitHalf<false>) + 14 * (kv.max_pages / 2 + 1)) / least + 1;
+  const long long blocks = ((long long)s.n_max * G + RP - 1) / RP, most = (long long)s.B * kv.Hkv * blocks * (2 * (wide ? kUnitHalf<true> : kUnitHalf<false>) + 15 * (kv.max_pages / 2 + 1)) / least + 1;
   const int grid = (int)(most < workgroups(wide) ? most : workgroups(wide));
   const uint32_t g_recip = G == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + G - 1) / G);
   int32_t* counters = (int32_t*)workspace;
