@@ -43,6 +43,7 @@ __device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
 // Measured in the wide kernel, 128 sequences of 1 .. 17 rows and 500 .. 32000 tokens, 7B heads: a step of up to 32, 64 and more rows 0.97, 1.25 and 2.27 us, a unit
 // besides its steps 10 us.  With 12 for the last, and 8 for both others, this batch took 227 us and 100 sequences around 3000 tokens 114; with 14 211 and 107, with 15 209
 // and 103; kUnitHalf 24, 28, 32, 36: 211, 210, 209, 211 and 106, 104, 103, 105.
+// Of the kernel for few rows 4, 8, 12: 64 x 1 row of 500 .. 32000 tokens 88, 86, 87 us; 1.5B heads, 256 x 1 .. 5 rows around 1500 tokens 79, 76, 76.
 constexpr int kSnap = 2;
 template <bool WIDE> constexpr int kUnitHalf = WIDE ? 32 : 8;             // on either side of a unit's steps
 template <bool WIDE> __device__ __forceinline__ int step_cost(int R) { return !WIDE ? 8 : R > 64 ? 15 : R > 32 ? 8 : 6; }
