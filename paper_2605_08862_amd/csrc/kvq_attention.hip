@@ -777,9 +777,10 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
 
 // Blocks of 32 rows on four waves, two workgroups on a CU, or of up to 128 rows on eight waves.  The second reads K/V once for four times the rows, but has
 // more to do before and behind its steps, so it needs many units (of 128 rows) and much to read; the block table's width is what the host knows of the lengths.
-// Narrow and wide, us: 7B heads, 17 rows, 32 units of 20000 tokens 72 and 82, 36 of 20000 123 and 84; 64 units of 1000 tokens (1024 pages) 23 and 29, 2800 (2816)
-// 38 and 39, 4000 (4032) 50 and 45, 8000 86 and 64; 9 rows, 512 units of 250 tokens (2560) 24 and 30, 500 (4096) 31 and 32, 1000 53 and 48; 1.5B heads, 9 rows, 128 units
-// of 1000 tokens (2048) 22 and 24, 2000 (4096) 31 and 28; prompts of 7B heads, 500 rows (896) 20 and 23, 1000 rows (3520) 41 and 34.
+// Narrow and wide, us: 7B heads, 17 rows, 32 units of 20000 tokens 69 and 80, 36 of 20000 122 and 80; 64 units of 1000 tokens (1024 pages) 22 and 27, 2800 (2816)
+// 38 and 38, 4000 (4032) 48 and 44, 8000 84 and 61; 512 units of 100 (1024) 29 and 27, 250 (2560) 39 and 36; 9 rows, 512 units of 250 tokens (2560) 23 and 28, 500 (4096) 30
+// and 30, 1000 52 and 45; 1.5B heads, 9 rows, 128 units of 1000 tokens (2048) 22 and 22, 2000 (4096) 30 and 26; prompts of 7B heads, 500 rows (896) 19 and 23, 1000
+// rows (3520) 40 and 33.
 constexpr int kWideUnits = 32, kWidePages = 2560;
 bool is_wide(int G, int q_max) { return (long long)q_max * G > 32; }
 bool runs_wide(const KvqView& kv, const KvqSeqs& s, int G) {
