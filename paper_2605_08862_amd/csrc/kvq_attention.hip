@@ -4,8 +4,8 @@
 // row, into equal shares, one for each workgroup (a multiple of the CUs).  Every workgroup finds its share from a prefix sum over the sequences that it makes
 // itself.  A share can begin and end inside a unit: the workgroup then leaves a partial (rows, maximum, sum), and the last of a unit's workgroups to arrive
 // merges them, in groups of four or eight where there are many (publish_arrival, common.h; nobody waits).
-//   * Up to 32 rows of a unit: four waves take a 32-token tile each of every step, with an online softmax of their own (attn_softmax.h), merged at the unit's end.
-//     More: eight waves, kvq_wide_kernel.
+//   * Few rows: blocks of 32, four waves take a 32-token tile each of every step, with an online softmax of their own (attn_softmax.h), merged at the unit's end.
+//     Many: blocks of 128, eight waves, kvq_wide_kernel.
 //   * S^T = K Q^T and O^T = V^T P^T on the 32 x 32 x 16 f16 MFMA.  A lane's sixteen bytes of codes are operands of two K-steps: one conversion with the block's
 //     scale gives two exact float16 values, so nothing is rounded that the 16-bit cache would not round.
 #include "kvq.h"
@@ -593,7 +593,7 @@ __device__ __forceinline__ void copy_to_lds(const uint8_t* src, char* dst) {
 // the memory pipeline copies it there (global -> LDS loads, a share of the 1 KiB pieces by each wave), NB buffers for each phase, NB - 1 tiles in flight and one
 // barrier per tile.
 // What bounds it: two query tiles, memory; four, that matrix and vector instructions of the two waves of a SIMD overlap in part only.  7B heads, 32 sequences of 8192
-// tokens (memory 57 us), 9 rows 66 us, 13 rows 90, 17 rows 100 .. 105.  Of the latter, with parts left out: the way to the first tile and the merges 22, copying the tiles
+// tokens (memory 57 us), 9 rows 65 us, 17 rows 98 .. 103.  Of the latter, at 105 then, with parts left out: the way to the first tile and the merges 22, copying the tiles
 // alone 69, matrix instructions alone 84 (half of their nominal rate, as a large matrix product has it too), everything but them 87, everything but the softmax 90,
 // everything but the conversions 100.  Two tiles per barrier, a tile of K read ahead, requests behind the scores: the same or slower; twelve waves with three phases:
 // 12 us more; scores of the next tile multiplied while this one's become probabilities: 10 us more; the two waves of a SIMD held half a tile apart by barriers: 10 us more;
