@@ -94,6 +94,17 @@ def test_logprobs(lib):
         assert B.bs_token_logprobs_workspace_bytes(*bad) == 0, bad
 
 
+def test_bind_without_a_context(lib):
+    assert lib.bs_kvq_bind_bytes(None) == 0 and lib.bs_kvq_bind(None, None, None, 0) == B.BS_EINVAL
+
+
+def test_temperatures_whose_reciprocal_overflows(lib):
+    need = B.bs_token_logprobs_workspace_bytes(1, 0, 100, 0)
+    call = lambda t: lib.bs_token_logprobs(1, 100, P, B.BS_F32, None, 0, P, None, t, 0, P, None, None, None, None, P, need, None)
+    assert all(call(t) == B.BS_EINVAL for t in (0.0, -1.0, 9e-39, 1e-45, float("inf"), float("nan")))
+    assert call(1e-38) == call(3e38) == B.BS_EHIP
+
+
 @pytest.fixture(scope="module")
 def assembly(tmp_path_factory):
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
