@@ -10,11 +10,10 @@
 //     scale gives two exact float16 values, so nothing is rounded that the 16-bit cache would not round.
 #include "kvq.h"
 #include "attn_softmax.h"
+#include "kvq_shares.h"
 #include <type_traits>
 
 namespace {
-
-constexpr int kStep = 4 * kTile;                       // tokens of a step: a tile for each wave
 
 struct KvqOut { void* p; int ld; };                    // ld > 0: float16 rows in chunk order (act_index); 0: bf16 [rows][Hq][D]
 
@@ -37,40 +36,6 @@ __device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
 }
 
 // ---- the shares ------------------------------------------------------------------------------------------------------------------
-// All units in a row (sequence, KV head, block) have a length: kUnitHalf, step_cost for each of their steps, kUnitHalf, in units of 1/8 step of a launch that is bound
-// by memory.  The workgroups cut that into W equal parts; a cut is moved to the next step's start, and to the unit's end or start where less than kSnap + 1
-// steps would be left on that side.  So a share is a run of steps, and what a unit costs besides its steps (its queries, the merge of the waves) counts.
-// Measured in the wide kernel, 128 sequences of 1 .. 17 rows and 500 .. 32000 tokens, 7B heads: a step of up to 32, 64 and more rows 0.97, 1.25 and 2.27 us, a unit
-// besides its steps 10 us.  With 12 for the last, and 8 for both others, this batch took 227 us and 100 sequences around 3000 tokens 114; with 14 211 and 107, with 15 209
-// and 103; kUnitHalf 24, 28, 32, 36: 211, 210, 209, 211 and 106, 104, 103, 105.
-// Of the kernel for few rows 4, 8, 12: 64 x 1 row of 500 .. 32000 tokens 88, 86, 87 us; 1.5B heads, 256 x 1 .. 5 rows around 1500 tokens 79, 76, 76.
-constexpr int kSnap = 2;
-template <bool WIDE> constexpr int kUnitHalf = WIDE ? 32 : 8;             // on either side of a unit's steps
-template <bool WIDE> __device__ __forceinline__ int step_cost(int R) { return !WIDE ? 8 : R > 64 ? 15 : R > 32 ? 8 : 6; }
-template <bool WIDE> constexpr int kBlock = WIDE ? 128 : 32;          // rows of a block
-// Query heads of a KV head.  x / g by a product with 2^32 / g rounded up: exact for x below 2^32 / g, i.e. any packed row.
-struct Group {
-  int g;
-  uint32_t recip;
-  __device__ __forceinline__ int div(int x) const { return g == 1 ? x : (int)__umulhi((uint32_t)x, recip); }
-};
-// Steps of the block qb of a sequence of n rows behind c tokens: of the tokens that its last row sees.
-template <int RP> __device__ __forceinline__ int block_steps(int c, int n, Group G, int qb) { return (c + min(n - 1, G.div((qb + 1) * RP - 1)) + kStep) / kStep; }
-
-struct Shares {
-  int total, W;                                         // length of everything, workgroups that have a share
-  unsigned long long per;                               // length of a share, 16 bits of fraction
-  float inv;                                            // its reciprocal
-  __device__ __forceinline__ int bound(int w) const { return w >= W ? total : (int)((w * per) >> 16); }
-  // the largest w with bound(w) <= p
-  __device__ __forceinline__ int of(int p) const {
-    int w = min(W - 1, (int)((float)p * inv));
-    while (w > 0 && bound(w) > p) --w;
-    while (w + 1 < W && bound(w + 1) <= p) ++w;
-    return w;
-  }
-};
-
 // A sequence that the thread which counted it leaves for the others: the one that this workgroup's share begins in.
 struct Seq { int b, n, c, slot; };
 // Sum over the lanes up to this one.
@@ -87,10 +52,9 @@ __device__ __forceinline__ int wave_scan(int v) {
 }
 
 // Called by all threads.  s_start, s_row [B + 1]: where every sequence begins, and its first packed row; s_scan: 2 words for each wave; s_seq: see above.
-// A share is no shorter than `least`, and longer than a step, so that every share between two others of a unit has a step of it.
 template <int THREADS, bool WIDE>
 __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add,
-                                              int n_max, int B, int n_slots, int max_pages, Group G, int Hkv, int least, int* s_start, int* s_row, int* s_scan, Seq* s_seq,
+                                              int n_max, int B, int n_slots, int max_pages, Group G, int Hkv, int* s_start, int* s_row, int* s_scan, Seq* s_seq,
                                               int32_t* __restrict__ status) {
   constexpr int NW = THREADS / 64, RP = kBlock<WIDE>;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -122,11 +86,7 @@ __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_sl
     if (w < wave) { bs += s_scan[w]; br += s_scan[NW + w]; }
     total += s_scan[w];
   }
-  Shares sh;
-  sh.total = __builtin_amdgcn_readfirstlane(total);
-  sh.W = __builtin_amdgcn_readfirstlane(min((int)gridDim.x, max(1, total / least)));
-  sh.per = (unsigned long long)((double)sh.total * 65536.0 / (double)sh.W);    // the same in every workgroup; (W - 1) per is below the total
-  sh.inv = (float)sh.W / (float)max(sh.total, 1);
+  const Shares sh = make_shares(__builtin_amdgcn_readfirstlane(total), (int)gridDim.x);
   const int p0 = sh.bound(blockIdx.x);
   const bool mine = bs <= p0 && p0 < bs + cost;
   if (mine && per == 1) *s_seq = Seq{at, n, c, slot};
@@ -142,27 +102,6 @@ __device__ __forceinline__ Shares find_shares(const int32_t* __restrict__ seq_sl
   return sh;
 }
 
-template <bool WIDE>
-struct Unit {
-  int b, h, qb, blocks;                                 // sequence, KV head, block of its blocks
-  int n, c, row0, slot;                                 // rows of the sequence, tokens before them, first packed row
-  int first, steps, step;                               // where the unit begins, its steps, what one costs
-  __device__ __forceinline__ int end() const { return first + 2 * kUnitHalf<WIDE> + step * steps; }
-  // step at which a cut at p is made
-  __device__ __forceinline__ int cut(int p) const {
-    const int x = max(p - first - kUnitHalf<WIDE>, 0) + step - 1, j = (int)__umulhi((uint32_t)x, step == 8 ? 536870912u : step == 15 ? 286331154u : 715827883u);   // / step
-    return p >= end() ? steps : p <= first + kUnitHalf<WIDE> + kSnap * step ? 0 : steps - j <= kSnap ? steps : j;
-  }
-  // the first and the last workgroup that have steps of the unit
-  __device__ __forceinline__ int first_share(const Shares& sh) const { return sh.of(min(first + kUnitHalf<WIDE> + kSnap * step, sh.total - 1)); }
-  __device__ __forceinline__ int last_share(const Shares& sh) const { return sh.of(first + kUnitHalf<WIDE> + max(step * (steps - kSnap - 1), kSnap * step)); }
-};
-template <bool WIDE>
-__device__ __forceinline__ void fill_unit(Unit<WIDE>& u, Group G) {
-  constexpr int RP = kBlock<WIDE>;
-  u.steps = block_steps<RP>(u.c, u.n, G, u.qb);
-  u.step = step_cost<WIDE>(u.n * G.g - u.qb * RP);
-}
 template <bool WIDE>
 __device__ __forceinline__ void enter_sequence(Unit<WIDE>& u, const int* s_start, const int* s_row, const int32_t* __restrict__ seq_slot, const int32_t* __restrict__ seq_pos, const int32_t* __restrict__ seq_n, int n_add, Group G) {
   u.b = __builtin_amdgcn_readfirstlane(u.b);
@@ -272,18 +211,18 @@ __device__ __forceinline__ void store_row(const KvqOut& out, int Hq, const Part&
 
 // ---- merge of a unit's parts -------------------------------------------------------------------------------------------------------
 // Partial rows: part_o [2 W][RP][D], and (maximum, sum) part_ml [kLevels][2 W][RP][2].  Parts are merged in groups of F neighbours by the last of a group to
-// arrive, into the place of the group's first part, the merged parts again, and so on: a unit of 64 parts of 119 rows is 4 MB, which one workgroup alone read in
+// arrive, into the place of the group's first part, the merged parts again, and so on (merge_levels): a unit of 64 parts of 119 rows is 4 MB, which one workgroup alone read in
 // 70 us of a launch of 88.  Maxima and sums of a level have a place of their own, since several threads read those of a row.
 // counters [kLevels][kMaxShares], zero between launches; a workgroup is the first of at most one group of more than one part on every level.
 constexpr int kLevels = 5, kMaxShares = 2 * kCUs;
 struct Parts { float *o, *ml; int32_t* counters; };
 template <int RP> constexpr uint32_t kMlLevel = (uint32_t)2 * kMaxShares * RP;      // rows of a level
 
-// Merges `count` parts, `stride` apart from part i0 of the unit on, on level `level`.  An item is four columns of a row; the loads of NI items and GC parts are in
+// Merges `count` parts, `stride` apart from part i0 of the unit on, on level `level` (merge_levels).  An item is four columns of a row; the loads of NI items and GC parts are in
 // flight together.
 template <int THREADS, int RP, int D, bool STEP, int NI, int GC>
-__device__ __forceinline__ void merge_group(const Part& un, const Parts& p, int level, int i0, int stride, int count, bool last, const KvqOut& out, int Hq, Group G,
-                                            int32_t* status) {
+__device__ __forceinline__ void merge_group(const Part& un, const Parts& p, int level, int i0, int stride, int count, int lone_level, bool last, const KvqOut& out,
+                                            int Hq, Group G, int32_t* status) {
   constexpr int CH = D / 4;
   const wt_buf bo = wt_buffer(p.o), bm = wt_buffer(p.ml);
   const int items = un.R * CH;
@@ -298,12 +237,12 @@ __device__ __forceinline__ void merge_group(const Part& un, const Parts& p, int 
       f32x4 v[GC][NI];
 #pragma unroll
       for (int u = 0; u < GC; ++u) {
-        const int i = i0 + min(c0 + u, count - 1) * stride;
-        const uint32_t row = partial_row<RP>(un.w_first + i, i == 0);
+        const int nth = min(c0 + u, count - 1), i = i0 + nth * stride;
+        const uint32_t row = partial_row<RP>(un.w_first + i, i == 0), ml_row = (nth == count - 1 ? lone_level : level) * kMlLevel<RP> + row;
 #pragma unroll
         for (int k = 0; k < NI; ++k) {                  // (an item behind the last one: the last one)
           const int it = min(it0 + k * THREADS, items - 1);
-          ml[u][k] = wt_load2(bm, (level * kMlLevel<RP> + row + it / CH) * 8);
+          ml[u][k] = wt_load2(bm, (ml_row + it / CH) * 8);
           v[u][k] = wt_load4(bo, ((row + it / CH) * D + it % CH * 4) * 4);
         }
       }
@@ -344,27 +283,14 @@ __device__ __forceinline__ void merge_group(const Part& un, const Parts& p, int 
 // Called by all threads of a workgroup that has stored its part of a cut unit on level 0.
 template <int THREADS, int RP, int D, bool STEP>
 __device__ __forceinline__ void merge_unit(const Part& un, const Parts& p, const KvqOut& out, int Hq, Group G, int32_t* status, int* s_flag) {
-  const bool few = un.R * (D / 4) <= THREADS;           // few rows, as of one long sequence
-  const int F = few ? 8 : 4, n = un.w_last - un.w_first + 1;
-  int i = (int)blockIdx.x - un.w_first;
-  for (int level = 0, stride = 1; stride < n; ++level, stride *= F) {
-    i -= i % (stride * F);
-    const int count = min(F, (n - i + stride - 1) / stride);
-    const bool last = stride * F >= n;
-    if (count > 1) {
-      if (!publish_arrival(p.counters + level * kMaxShares + un.w_first + i, count, s_flag)) return;
-      if (count == 2 && !few) merge_group<THREADS, RP, D, STEP, 8, 2>(un, p, level, i, stride, count, last, out, Hq, G, status);
-      else if (few) merge_group<THREADS, RP, D, STEP, 1, 8>(un, p, level, i, stride, count, last, out, Hq, G, status);
-      else merge_group<THREADS, RP, D, STEP, 4, 4>(un, p, level, i, stride, count, last, out, Hq, G, status);
-    } else {                                            // nothing to merge with on this level
-      const wt_buf bm = wt_buffer(p.ml);
-      const uint32_t row = partial_row<RP>(un.w_first + i, i == 0);
-      for (int r = threadIdx.x; r < un.R; r += THREADS) {
-        const wt_f32x2 ml = wt_load2(bm, (level * kMlLevel<RP> + row + r) * 8);
-        wt_store2(bm, ((level + 1) * kMlLevel<RP> + row + r) * 8, ml[0], ml[1]);
-      }
-    }
-  }
+  const bool few = un.R * (D / 4) <= THREADS;           // few rows, as of one long sequence: groups of eight
+  merge_levels((int)blockIdx.x - un.w_first, un.w_last - un.w_first + 1, few ? 3 : 2,
+               [&](int level, int i, int count) { return publish_arrival(p.counters + level * kMaxShares + un.w_first + i, count, s_flag); },
+               [&](int level, int i, int stride, int count, int lone_level, bool last) {
+                 if (count == 2 && !few) merge_group<THREADS, RP, D, STEP, 8, 2>(un, p, level, i, stride, count, lone_level, last, out, Hq, G, status);
+                 else if (few) merge_group<THREADS, RP, D, STEP, 1, 8>(un, p, level, i, stride, count, lone_level, last, out, Hq, G, status);
+                 else merge_group<THREADS, RP, D, STEP, 4, 4>(un, p, level, i, stride, count, lone_level, last, out, Hq, G, status);
+               });
 }
 
 // Online softmax of one tile of scores (attn_softmax.h): the scores become probabilities in float16, the running maximum, sum and accumulators follow.
@@ -424,7 +350,7 @@ template <bool STEP> __device__ __forceinline__ u32x4 query8(u32x4 v, bool& rang
   const int32_t *__restrict__ seq_slot, const int32_t *__restrict__ seq_pos, const int32_t *__restrict__ seq_n, int n_add, int n_max, int B,                \
       const int32_t *__restrict__ block_table, int n_slots, int max_pages, int n_pages, const uint8_t *__restrict__ k_pages, const uint8_t *__restrict__ v_pages, \
       const float *__restrict__ k_scale, const float *__restrict__ v_scale, int Hq, int Hkv, int g_n, uint32_t g_recip, float scale_log2e, const uint16_t *__restrict__ q, size_t q_stride, \
-      KvqOut out, int least, Parts parts, int32_t *__restrict__ status
+      KvqOut out, Parts parts, int32_t *__restrict__ status
 
 // Blocks of up to 32 rows, four waves, two workgroups on a CU.  STEP: inside bs_verify_step (float16 queries, output in chunk order).  Every wave has two tiles of K
 // and V codes in registers and loads the next but one behind the products that read them.
@@ -446,7 +372,7 @@ __global__ void __launch_bounds__(256, 2) kvq_attention_kernel(BS_KVQ_PARAMS) {
   const int tid = threadIdx.x, w_id = blockIdx.x;
   const Group G{g_n, g_recip};
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, ln = lane & 31, lg = lane >> 5;
-  const Shares sh = find_shares<256, false>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, least, s_start, s_row, s_scan, &s_seq, status);
+  const Shares sh = find_shares<256, false>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, s_start, s_row, s_scan, &s_seq, status);
   for_parts<false>(sh, B, s_start, s_row, seq_slot, seq_pos, seq_n, n_add, G, Hkv, s_seq, [&](const Part& un) {
     const int32_t* __restrict__ bt = block_table + (size_t)un.slot * max_pages;
     const int t0 = 4 * un.s_lo + wave, t_end = min(4 * un.s_hi, un.n_tiles);
@@ -618,7 +544,7 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
   const int tid = threadIdx.x, w_id = blockIdx.x;
   const Group G{g_n, g_recip};
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, ln = lane & 31, lg = lane >> 5;
-  const Shares sh = find_shares<512, true>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, least, s_start, s_row, s_scan, &s_seq, status);
+  const Shares sh = find_shares<512, true>(seq_slot, seq_pos, seq_n, n_add, n_max, B, n_slots, max_pages, G, Hkv, s_start, s_row, s_scan, &s_seq, status);
 
   auto run = [&](auto nqt_tag, const Part& un) {
     constexpr int NQT = decltype(nqt_tag)::value, NPH = 8 / NQT;
@@ -775,32 +701,18 @@ __global__ void __launch_bounds__(512) kvq_wide_kernel(BS_KVQ_PARAMS) {
   });
 }
 
-// Blocks of 32 rows on four waves, two workgroups on a CU, or of up to 128 rows on eight waves.  The second reads K/V once for four times the rows, but has
-// more to do before and behind its steps, so it needs many units (of 128 rows) and much to read; the block table's width is what the host knows of the lengths.
-// Narrow and wide, us: 7B heads, 17 rows, 32 units of 20000 tokens 69 and 80, 36 of 20000 122 and 80; 64 units of 1000 tokens (1024 pages) 22 and 27, 2800 (2816)
-// 38 and 38, 4000 (4032) 48 and 44, 8000 84 and 61; 512 units of 100 (1024) 29 and 27, 250 (2560) 39 and 36; 9 rows, 512 units of 250 tokens (2560) 23 and 28, 500 (4096) 30
-// and 30, 1000 52 and 45; 1.5B heads, 9 rows, 128 units of 1000 tokens (2048) 22 and 22, 2000 (4096) 30 and 26; prompts of 7B heads, 500 rows (896) 19 and 23, 1000
-// rows (3520) 40 and 33.
-constexpr int kWideUnits = 32, kWidePages = 2560;
-bool is_wide(int G, int q_max) { return (long long)q_max * G > 32; }
-bool runs_wide(const KvqView& kv, const KvqSeqs& s, int G) {
-  const long long units = s.B * kv.Hkv * (((long long)s.n_max * G + 127) / 128);
-  return is_wide(G, s.n_max) && units > kWideUnits && units * kv.max_pages > kWidePages;
-}
-int workgroups(bool wide) { return (wide ? 1 : 2) * kCUs; }
 size_t workspace_bytes(bool wide, int D) {
   const size_t rows = (size_t)2 * (wide ? 128 : 32);
-  return kLevels * kMaxShares * sizeof(int32_t) + rows * sizeof(float) * (kLevels * kMaxShares * 2 + (size_t)workgroups(wide) * D);
+  return kLevels * kMaxShares * sizeof(int32_t) + rows * sizeof(float) * (kLevels * kMaxShares * 2 + (size_t)share_workgroups(wide) * D);
 }
 
 template <int D, bool STEP>
 void launch(const KvqView& kv, const KvqSeqs& s, int Hq, const void* q, size_t q_stride, KvqOut out, int32_t* status, void* workspace, hipStream_t st) {
-  const bool wide = runs_wide(kv, s, Hq / kv.Hkv);
-  const int RP = wide ? 128 : 32, G = Hq / kv.Hkv, least = 32;
-  // no more workgroups than shares, of sequences as long as the block table is wide
-  const long long blocks = ((long long)s.n_max * G + RP - 1) / RP, most = (long long)s.B * kv.Hkv * blocks * (2 * (wide ? kUnitHalf<true> : kUnitHalf<false>) + 15 * (kv.max_pages / 2 + 1)) / least + 1;
-  const int grid = (int)(most < workgroups(wide) ? most : workgroups(wide));
-  const uint32_t g_recip = G == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + G - 1) / G);
+  const int G = Hq / kv.Hkv;
+  const bool wide = runs_wide(s.B, kv.Hkv, (long long)s.n_max * G, kv.max_pages);
+  const int RP = wide ? 128 : 32;
+  const int grid = share_grid(wide, s.B, kv.Hkv, (long long)s.n_max * G, kv.max_pages);
+  const uint32_t g_recip = make_group(G).recip;
   int32_t* counters = (int32_t*)workspace;
   float* ml = (float*)(counters + kLevels * kMaxShares);
   const Parts parts{ml + (size_t)kLevels * 2 * kMaxShares * RP * 2, ml, counters};
@@ -812,12 +724,12 @@ void launch(const KvqView& kv, const KvqSeqs& s, int Hq, const void* q, size_t q
   (void)set;
   const float scale_log2e = 1.4426950408889634f / sqrtf((float)D);
   hipLaunchKernelGGL(kern, dim3(grid), dim3(wide ? 512 : 256), lds, st, s.slot, s.pos, s.n, s.n_add, s.n_max, s.B, kv.block_table, kv.n_slots, kv.max_pages, kv.n_pages,
-                     kv.k, kv.v, kv.ks, kv.vs, Hq, kv.Hkv, G, g_recip, scale_log2e, (const uint16_t*)q, q_stride, out, least, parts, status);
+                     kv.k, kv.v, kv.ks, kv.vs, Hq, kv.Hkv, G, g_recip, scale_log2e, (const uint16_t*)q, q_stride, out, parts, status);
 }
 }  // namespace
 
 size_t kvq_attention_workspace(int Hq, int Hkv, int D, int q_max) {
-  const size_t few = workspace_bytes(false, D), many = is_wide(Hq / Hkv, q_max) ? workspace_bytes(true, D) : 0;
+  const size_t few = workspace_bytes(false, D), many = is_wide((long long)q_max * (Hq / Hkv)) ? workspace_bytes(true, D) : 0;
   return few > many ? few : many;
 }
 
