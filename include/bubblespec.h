@@ -290,7 +290,7 @@ typedef struct {
 
 /* Writes rows [n, n_kv_heads, head_dim] bf16 (row_stride elements from one row to the next, at least n_kv_heads * head_dim) to
  * positions pos0[b] .. pos0[b] + n_rows[b] of slot seq_slot[b], n_rows[b] <= n_max.  Positions before pos0 must have been written,
- * positions behind the last row become undefined.  Of sequences with the same slot only the first is written (BS_FAULT_SLOT); pages that
+ * positions behind the last row become undefined.  Of sequences with rows and the same slot only the first is written (BS_FAULT_SLOT); pages that
  * slots share must not be written through two of them at once.
  * Errors: BS_EINVAL (null, misaligned pages), BS_ESHAPE (head_dim not in {64, 128}, n_kv_heads outside [1, 256], B outside
  * [1, 4096], n_max outside [1, max_pages_per_seq * BS_PAGE_TOKENS], row_stride too small, a launch of more than 2^23 pages), BS_EHIP. */

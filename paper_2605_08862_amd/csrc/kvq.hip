@@ -7,7 +7,7 @@ namespace {
 struct Span { int page, lo, hi, row; bool live; };
 
 // The sequence's rows are checked as a whole, by every workgroup that has a page of it alike: a sequence with a bad count, slot, position or page, or
-// (writes) with the slot of an earlier sequence, is skipped.  s_red: one word per wave.
+// (writes) with the slot of an earlier sequence that has rows, is skipped.  s_red: one word per wave.
 template <bool WRITE>
 __device__ __forceinline__ Span find_span(const KvqView& kv, const KvqSeqs& q, int b, int page_at, int* s_red, int32_t* status) {
   Span sp{0, 0, 0, 0, false};
@@ -29,8 +29,10 @@ __device__ __forceinline__ Span find_span(const KvqView& kv, const KvqSeqs& q, i
     for (int p = first + (int)threadIdx.x; p <= last; p += 256) if ((unsigned)bt[p] >= (unsigned)kv.n_pages) bad |= BS_FAULT_KV_PAGES;
   if (q.slot)
     for (int c = threadIdx.x; c < b; c += 256) {
-      if (!q.row_start) { const int m = q.n[c] + q.n_add; before += m >= 0 && m <= q.n_max ? m : 0; }
-      if (WRITE && q.slot[c] == slot) bad |= BS_FAULT_SLOT;
+      const int m = WRITE || !q.row_start ? q.n[c] + q.n_add : 0;
+      const bool rows = m > 0 && m <= q.n_max;           // (a padded entry may have any slot)
+      before += rows ? m : 0;
+      if (WRITE && rows && q.slot[c] == slot) bad |= BS_FAULT_SLOT;
     }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) { before += __shfl_xor(before, o); bad |= __shfl_xor(bad, o); }

@@ -428,3 +428,25 @@ def test_pages_behind_four_gib():
         got, want = (c.attention(0, q[:rows * len(slots)], *args).double() for c in (big, small))
         assert bool((got - want).abs().max() <= 2.0 ** -6 * want.abs().max()), (len(slots), rows)
     assert big.poll_status() == 0 and small.poll_status() == 0
+
+
+@pytest.mark.parametrize("pad", [0, -1, 9], ids=["empty", "bad_count_low", "bad_count_high"])
+def test_a_padded_entry_in_front_of_its_slot(pad):
+    """An entry without rows, or with a count that is refused and so has none, takes no slot from those behind it."""
+    rng = np.random.default_rng(pad + 50)
+    H, D = 2, 64
+    x = Both(H, H, D, [130, 130, 130], 1)
+    k, v = _rows(rng, 12, H, D), _rows(rng, 12, H, D)
+    slots, pos, counts = [1, 0, 1, 2, 0, 2], [50, 7, 0, 64, 0, 3], [pad, pad, 5, pad, 4, 3]
+    x.cache.write(0, _i32(slots), _i32(pos), _i32(counts), 8, k.to(DEV), v.to(DEV))
+    assert x.cache.poll_status() == (B.BS_FAULT_DRAFT_LEN if pad else 0)
+    at = 0
+    for s, p, n in zip(slots, pos, counts):
+        if n != pad:
+            x.k[s].write(p, k[at:at + n].double().numpy())
+            x.v[s].write(p, v[at:at + n].double().numpy())
+            x.len[s] = p + n
+            at += n
+    x.check()
+    x.write([1, 1, 2], [5, 9, 6], [3, 0, 1], k[:4], v[:4])                   # padding behind the real entry
+    x.check()
