@@ -55,6 +55,7 @@ struct bs_ctx {
   float* filter_logits = nullptr;   // bf16 models: caller's [M_max, V] float32 scratch for the filtered path
   // 8-bit cache (bs_kvq_bind): one view per layer, staging pages of a step's rows, attention workspace
   std::vector<KvqView> kvq;
+  bool kvq_only = false;      // the context's 16-bit pages are (or were) pages of an 8-bit cache, half as large: no step may run without one bound
   void *kvq_k = nullptr, *kvq_v = nullptr, *kvq_ws = nullptr;
   bool unfused_qkv = false;   // test hook: QKV GEMM + separate rotary kernel instead of the fused kernel
   std::vector<hipEvent_t> prof_ev;     // pairs (start, stop), created on first use
@@ -833,7 +834,12 @@ size_t bs_kvq_bind_bytes(const bs_ctx* c) {
 }
 bs_status bs_kvq_bind(bs_ctx* c, const bs_kvq_desc* layers, void* workspace, size_t workspace_bytes) {
   if (!c) return BS_EINVAL;
-  if (!layers) { c->kvq.clear(); c->verify_pending = false; return BS_OK; }
+  if (!layers) {
+    if (c->kvq_only) return fail(c, BS_ESTATE, "bs_kvq_bind: the context has no 16-bit pages to go back to");
+    c->kvq.clear();
+    c->verify_pending = false;
+    return BS_OK;
+  }
   if (c->s.dtype != BS_BF16) return fail(c, BS_EINVAL, "bs_kvq_bind: float32 models have no 8-bit cache");
   if (!kvq_heads_ok(c->s.Hq, c->s.Hkv, c->s.D)) return fail(c, BS_ESHAPE, "bs_kvq_bind: heads that bs_kvq_attention does not take");
   if (!workspace || ((uintptr_t)workspace & 255)) return fail(c, BS_EINVAL, "bs_kvq_bind: workspace null or not on 256 bytes");
@@ -847,13 +853,18 @@ bs_status bs_kvq_bind(bs_ctx* c, const bs_kvq_desc* layers, void* workspace, siz
   }
   if (!kvq_attention_counts(c->B_max, c->s.Hkv, c->s.Hq / c->s.Hkv, c->kv.max_pages, c->k_max + 1)) return fail(c, BS_ESHAPE, "bs_kvq_bind: too many tokens");
   if (workspace_bytes < bs_kvq_bind_bytes(c)) return fail(c, BS_ECAPACITY, "bs_kvq_bind: workspace too small");
-  c->kvq.clear();
+  std::vector<KvqView> views;
   try {
-    c->kvq.reserve(c->s.L);
+    views.reserve(c->s.L);
   } catch (const std::bad_alloc&) {
     return fail(c, BS_ECAPACITY, "bs_kvq_bind: out of host memory");
   }
-  for (int l = 0; l < c->s.L; ++l) c->kvq.push_back(view_of(layers[l]));
+  for (int l = 0; l < c->s.L; ++l) {
+    views.push_back(view_of(layers[l]));
+    for (int i = 0; i < c->s.L; ++i)
+      if (c->k_pages[i] == layers[l].k_pages || c->k_pages[i] == layers[l].v_pages || c->v_pages[i] == layers[l].k_pages || c->v_pages[i] == layers[l].v_pages) c->kvq_only = true;
+  }
+  c->kvq.swap(views);
   kvq_bind_carve(c, (char*)workspace, &c->kvq_k, &c->kvq_v, &c->kvq_ws);
   c->verify_pending = false;
   return BS_OK;

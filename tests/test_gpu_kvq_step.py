@@ -11,7 +11,7 @@ from oracle import decoder as OD
 from oracle import logprobs as OL
 from paper_2605_08862_amd import binding as B
 from paper_2605_08862_amd import workloads as W
-from paper_2605_08862_amd.runtime import Engine, LogprobScorer, fuse_weights
+from paper_2605_08862_amd.runtime import Engine, KvqCache, LogprobScorer, fuse_weights
 from tests import helpers as H
 
 pytestmark = pytest.mark.gpu
@@ -208,3 +208,24 @@ def test_bind_and_unbind():
     with pytest.raises(B.BsError) as e:
         Engine(tiny, fuse_weights(W.make_weights(tiny, seed=1), tiny["dtype"], DEV), 1, 64, B_max=1, k_max=0, kv_bits=8)
     assert e.value.status == B.BS_EINVAL
+
+
+def test_a_context_without_16_bit_pages_stays_bound():
+    """Engine(kv_bits=8) gives bs_create the pages of the 8-bit cache, which are half as large: no step may take them for 16-bit ones."""
+    desc = SHAPES["d128_g3"]
+    eng, _ = _engine(desc, 1, [100, 100], 3)
+    args = (H.dev_i32([0, 1]), H.dev_i32([5, 6]), H.dev_i32([[1, 2, 3], [4, 5, 6]]), H.dev_i32([3, 1]), 3)
+    want = eng.verify_step(*args, want_logits=True)
+
+    def refused(status, *call):
+        with pytest.raises(B.BsError) as e:
+            B.bs_kvq_bind(eng.ctx, *call)
+        assert e.value.status == status
+    refused(B.BS_ESTATE, None, None)
+    refused(B.BS_ECAPACITY, eng.kvq.desc, eng._kvq_workspace[:256])
+    assert torch.equal(eng.verify_step(*args, want_logits=True), want)     # bound as before
+    other = KvqCache(desc["n_layers"], desc["n_q_heads"], desc["n_kv_heads"], desc["head_dim"], 2, 100, 4, device=DEV, block_table=eng.block_table, n_pages=eng.n_pages)
+    B.bs_kvq_bind(eng.ctx, other.desc, eng._kvq_workspace)                 # another cache of the same sizes may take its place
+    assert torch.equal(eng.verify_step(*args, want_logits=True), want)
+    refused(B.BS_ESTATE, None, None)
+    assert torch.equal(eng.verify_step(*args, want_logits=True), want) and eng.poll_status() == 0
