@@ -5,6 +5,7 @@ import subprocess
 
 import pytest
 
+from tests.test_gpu_kvq_kernels import CASES as KERNEL_CASES, IDS as KERNEL_IDS
 from tests.test_gpu_kvq_merge import CASES, IDS
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -47,3 +48,11 @@ def test_the_cases_of_the_gpu_test_reach_their_merges(program, case):
         few = rows * (D // 4) <= threads
         reached |= {(few, level) for level in _lone_levels(parts, 8 if few else 4)}
     assert wanted <= reached, (wanted, reached, out)
+
+
+@pytest.mark.parametrize("case", KERNEL_CASES, ids=KERNEL_IDS)
+def test_the_cases_of_both_kernels_run_them(program, case):
+    Hq, Hkv, D, ctx, counts, besides = case
+    longest = max(c + n for c, n in zip(ctx, counts))
+    for wide, most in ((1, max(longest, besides)), (0, longest)):
+        program(wide, Hkv, Hq // Hkv, max(counts), -(-most // 64), *[v for pair in zip(ctx, counts) for v in pair])
