@@ -278,7 +278,8 @@ bs_status bs_kv_read(bs_ctx* ctx, int layer, int slot, int pos0, int n, void* k_
  * clears; BS_FAULT_* bits are or-ed into it; may be NULL).  Rows are packed in batch order: sequence b has n[b] rows, which start
  * at sum_{b'<b} n[b'] (a count outside [0, n_max] sets BS_FAULT_DRAFT_LEN and counts as 0).  A sequence with a bad slot
  * (BS_FAULT_SLOT), or with positions or page ids outside the cache (BS_FAULT_KV_PAGES), is skipped: its rows of the outputs and
- * its pages stay as they are (attention: rows that see a bad page id).  A sequence without rows is skipped whatever its slot is (padded batches). */
+ * its pages stay as they are.  (Attention, a bad page id: the rows that see it stay as they are; those before them may, too.)  A sequence without rows is
+ * skipped whatever its slot is (padded batches). */
 typedef struct {
   int32_t n_pages, n_slots, max_pages_per_seq, n_kv_heads, head_dim;
   void* k_pages;              /* dev [n_pages] pages of n_kv_heads * BS_PAGE_TOKENS * head_dim bytes, 16-byte aligned; element  */

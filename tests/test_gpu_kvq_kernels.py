@@ -1,9 +1,10 @@
 """Attention over the 8-bit cache by each of its two kernels on the same batches (which one runs follows from the number of units and the width of the block
-table: a slot of its own makes the table wide)."""
+table: a slot of its own makes the table wide), and pages whose ids are bad for some rows of a sequence only."""
 import numpy as np
 import pytest
 import torch
 
+from paper_2605_08862_amd import binding as B
 from paper_2605_08862_amd.runtime import KvqCache
 from tests.test_gpu_kvq import DEV, Both, _close_on_gpu, _i32
 
@@ -55,3 +56,32 @@ def test_each_kernel_matches_the_oracle(case, wide):
     x.cache.attention(0, (q.float().flip(0) * -3.0).to(torch.bfloat16), *args, out=out)
     x.cache.attention(0, q, *args, out=out)
     assert torch.equal(out, first) and bool((out[M:] == 7.0).all()) and x.cache.poll_status() == 0
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,ctx,counts,page,besides", [
+    (28, 4, 128, [30, 100], [9, 300], 5, 0),                               # rows 0 .. 219 of a piece of a prompt do not see its page 5
+    (28, 4, 128, [30, 100], [9, 300], 5, 40000),
+    (28, 4, 64, [30, 100], [9, 300], 1, 40000),                            # a page that every row sees
+    (12, 2, 128, [9000, 70], [1, 17], 1, 0),                               # every row of a verify block sees it
+    (12, 2, 128, [9000, 120], [1, 17], 2, 0),                              # rows 8 .. 16 of one block see page 2
+    (28, 4, 128, [9000, 9020], [1, 17], 141, 0),                           # a unit cut into parts: rows 4 .. 16
+    (28, 4, 128, [60] * 40 + [10000], [9] * 40 + [300], 160, 0),           # the same in the kernel for many rows
+], ids=str)
+def test_rows_beside_a_bad_page(Hq, Hkv, D, ctx, counts, page, besides):
+    """Rows that see the page stay as they are; of those before them, and of the other sequences, what is written is right."""
+    x, slots, q = _filled_in(Hq, Hkv, D, ctx, counts, 3, besides)
+    args = (_i32(slots), _i32(ctx), _i32(counts), max(counts))
+    b, clean = len(ctx) - 1, x.cache.attention(0, q, *args)
+    seen = max(0, min(counts[b], page * 64 - ctx[b]))                      # rows below the page
+    table, kept = x.cache.block_table, int(x.cache.block_table[slots[b], page])
+    for bad in (-1, x.cache.n_pages):
+        out = torch.full_like(q, 3.0)
+        table[slots[b], page] = bad
+        x.cache.attention(0, q, *args, out=out)
+        assert x.cache.poll_status() == (B.BS_FAULT_KV_PAGES if seen < counts[b] else 0)
+        table[slots[b], page] = kept
+        first = sum(counts[:b])
+        assert bool((out[first + seen:] == 3.0).all())
+        left = (out == 3.0).all(-1, keepdim=True)
+        assert not bool(left[:first].any())
+        _close_on_gpu(x, torch.where(left, clean, out), q, slots, ctx, counts[:b] + [seen])
