@@ -229,3 +229,29 @@ def test_a_context_without_16_bit_pages_stays_bound():
     assert torch.equal(eng.verify_step(*args, want_logits=True), want)
     refused(B.BS_ESTATE, None, None)
     assert torch.equal(eng.verify_step(*args, want_logits=True), want) and eng.poll_status() == 0
+
+
+SHAPES["d64_g4"] = W.shape("mini_bf16", n_q_heads=8, n_kv_heads=2, head_dim=64)
+
+
+@pytest.mark.parametrize("shape,ctx,k_b,k_max,besides", [
+    ("d128_g7", [300, 40, 129, 0] * 9, [16, 3, 9, 14] * 9, 16, 5000),      # a wide block table: the attention kernel for many rows
+    ("d64_g4", [90, 0, 300, 64] * 5, [16, 3, 0, 9] * 5, 16, 5000),
+    ("d128_g3", [4300], [0], 0, 0),                                        # units cut into parts, merged in several levels
+    ("d128_g3", [9000, 70], [8, 2], 8, 0),
+    ("d128_g7", [9000], [16], 16, 0),
+    ("d64_g4", [7000, 5], [4, 4], 4, 0),
+])
+def test_steps_of_many_rows_and_long_contexts(shape, ctx, k_b, k_max, besides):
+    """As above: the slot `besides` only makes the block table wide."""
+    desc = SHAPES[shape]
+    rng = np.random.default_rng(sum(ctx) + k_max)
+    n = len(ctx)
+    eng, wn = _engine(desc, 22, [c + 2 * (k_max + 1) for c in ctx] + [max(besides, 1)], k_max, B_max=n)
+    for b in range(n):
+        if ctx[b]:
+            for l, (k, v) in enumerate(W.context_kv(desc, ctx[b], 300 + b)):
+                eng.kv_write(l, b, 0, k.to(DEV), v.to(DEV))
+    eng.ctx_len[:n].copy_(H.dev_i32(ctx))
+    slots = [int(s) for s in rng.permutation(n)]
+    _step(eng, wn, H.oracle_desc(desc), slots, [ctx[s] for s in slots], [k_b[s] for s in slots], k_max, rng)
