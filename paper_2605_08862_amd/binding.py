@@ -313,7 +313,13 @@ def _rows(t, width, dev):
 
 def make_kvq_desc(kv):
     """kv: dict(n_pages, n_slots, max_pages_per_seq, n_kv_heads, head_dim, and the tensors k_pages, v_pages (uint8), k_scale,
-    v_scale (float32), block_table).  The description holds addresses only: the caller keeps the tensors."""
+    v_scale (float32), block_table (int32)).  The description holds addresses only: the caller keeps the tensors."""
+    blocks, places = kv["n_pages"] * kv["n_kv_heads"], kv["n_slots"] * kv["max_pages_per_seq"]
+    for name, dtype, n in (("k_pages", torch.uint8, blocks * BS_PAGE_TOKENS * kv["head_dim"]), ("v_pages", torch.uint8, blocks * BS_PAGE_TOKENS * kv["head_dim"]),
+                           ("k_scale", torch.float32, blocks), ("v_scale", torch.float32, blocks), ("block_table", torch.int32, places)):
+        t = kv[name]
+        if t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or t.device != kv["block_table"].device:
+            raise BsError(BS_EINVAL, "make_kvq_desc: %s must be dense, %s, with at least %d elements, and on one device with the others" % (name, dtype, n))
     return bs_kvq_desc(kv["n_pages"], kv["n_slots"], kv["max_pages_per_seq"], kv["n_kv_heads"], kv["head_dim"], kv["k_pages"].data_ptr(),
                        kv["v_pages"].data_ptr(), kv["k_scale"].data_ptr(), kv["v_scale"].data_ptr(), kv["block_table"].data_ptr())
 

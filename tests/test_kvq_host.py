@@ -144,3 +144,16 @@ def test_requests_of_the_shared_tiles_are_counted_right(assembly):
     assert len(loops) == 8
     for D, n, ops in loops:
         assert ops == ["global_load_lds_dword"] + ["global_load_lds_dwordx4"] * expected[D, n], (D, n, ops)
+
+
+def test_a_cache_of_other_tensors_is_not_described():
+    kv = dict(n_pages=5, n_slots=2, max_pages_per_seq=3, n_kv_heads=2, head_dim=64, k_pages=torch.zeros(5, 2 * 64 * 64, dtype=torch.uint8), v_pages=torch.zeros(5 * 2 * 64 * 64, dtype=torch.uint8),
+              k_scale=torch.zeros(5, 2), v_scale=torch.zeros(5, 2), block_table=torch.zeros(2, 3, dtype=torch.int32))
+    d = B.make_kvq_desc(kv)
+    assert d.k_pages == kv["k_pages"].data_ptr() and d.block_table == kv["block_table"].data_ptr() and d.n_pages == 5
+    for name in ("k_pages", "v_pages", "k_scale", "v_scale", "block_table"):
+        t = kv[name]
+        for bad in (t.flatten()[:-1], t.to(torch.int64), t.to(torch.bfloat16), torch.cat([t, t])[::2], t.to("meta")):
+            with pytest.raises(B.BsError) as e:
+                B.make_kvq_desc(dict(kv, **{name: bad}))
+            assert e.value.status == B.BS_EINVAL, name
