@@ -292,6 +292,13 @@ def _ints(t, n, dev):
     return _here(t, dev)
 
 
+def _floats(t, n, dev):
+    """Address of at least n float32 words on device `dev` (None: NULL; an address: itself)."""
+    if t is not None and type(t) is not int and (t.dtype is not torch.float32 or t.numel() < n):
+        raise BsError(BS_EINVAL, "%d float32 words are expected, not %d of %s" % (n, t.numel(), t.dtype))
+    return _here(t, dev)
+
+
 def _rows(t, width, dev):
     """(address, elements from one row to the next) of packed rows [n, ..., ...] whose inner dimensions are dense."""
     if t.dtype is _BF16 and t.get_device() == dev and t.is_contiguous() and t.shape[0] * width == t.numel():
@@ -386,10 +393,14 @@ def bs_token_logprobs(B, vocab, logits, draft_len, k_max, tokens, n_tokens, temp
         workspace_bytes = workspace.numel() * workspace.element_size()
     if logits.shape[-1] != vocab:
         raise BsError(BS_ESHAPE, "bs_token_logprobs: rows of %d logits, %d expected" % (logits.shape[-1], vocab))
+    entries = B * (k_max + 1)
+    if draft_len is None and logits.numel() < entries * vocab:
+        raise BsError(BS_ESHAPE, "bs_token_logprobs: fewer rows of logits than tokens")
     dev = torch.cuda.current_device()
     dtype = BS_F32 if logits.dtype == torch.float32 else BS_BF16 if logits.dtype == torch.bfloat16 else -1
-    st = lib().bs_token_logprobs(B, vocab, _here(logits, dev), dtype, _ints(draft_len, B, dev), k_max, _ints(tokens, B * (k_max + 1), dev), _ints(n_tokens, B, dev), temperature, n_top,
-                                 _here(logprob, dev), _here(entropy, dev), _here(top_tokens, dev), _here(top_logprobs, dev), _here(status, dev),
+    st = lib().bs_token_logprobs(B, vocab, _here(logits, dev), dtype, _ints(draft_len, B, dev), k_max, _ints(tokens, entries, dev), _ints(n_tokens, B, dev), temperature, n_top,
+                                 _floats(logprob, entries, dev), _floats(entropy, entries, dev), _ints(top_tokens, entries * n_top, dev), _floats(top_logprobs, entries * n_top, dev),
+                                 _ints(status, 1, dev),
                                  _here(workspace, dev), workspace_bytes, _stream())
     if st != BS_OK:
         raise BsError(st, "bs_token_logprobs")

@@ -258,8 +258,6 @@ class LogprobScorer:
             raise B.BsError(B.BS_ESHAPE, "LogprobScorer: sizes exceed those of the workspace")
         if logits.get_device() != self._index:
             raise B.BsError(B.BS_EINVAL, "LogprobScorer: logits on %s, workspace on %s" % (logits.device, self.device))
-        if draft_len is None and logits.shape[0] < n * width:
-            raise B.BsError(B.BS_ESHAPE, "LogprobScorer: fewer rows of logits than tokens")
         lp = torch.empty((n, width), device=self.device)
         h = torch.empty_like(lp)
         out, at = {"logprob": lp, "entropy": h}, (None, None)

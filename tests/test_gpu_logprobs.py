@@ -197,3 +197,24 @@ def test_python_checks():
         with pytest.raises(B.BsError):
             call()
     assert s.poll_status() == 0
+
+
+def test_outputs_of_another_type_or_too_short_are_refused():
+    V, n_top = 100, 3
+    z, tokens = torch.zeros(4, V, device=DEV), _i32([[1, 2], [3, 4]])
+    f, i = lambda *shape: torch.full(shape, 5.0, device=DEV), lambda *shape: torch.full(shape, 5, dtype=torch.int32, device=DEV)
+    s = LogprobScorer(2, 1, V, n_top, device=DEV)
+    good = dict(logprob=f(2, 2), entropy=f(2, 2), top_tokens=i(2, 2, 3), top_logprobs=f(2, 2, 3), status=i(1).zero_())
+    call = lambda **over: B.bs_token_logprobs(2, V, z, None, 1, tokens, None, 1.0, n_top, **{**good, **over}, workspace=s.workspace)
+    call()
+    kept = {k: v.clone() for k, v in good.items()}
+    for name, t in good.items():
+        bad = [t.flatten()[:-1], t.cpu(), t.double() if t.is_floating_point() else t.long(), t.bfloat16()]
+        if t.dim() > 1:
+            bad.append(t.transpose(0, 1))
+        for b in bad:
+            with pytest.raises(B.BsError):
+                call(**{name: b})
+    with pytest.raises(B.BsError):
+        B.bs_token_logprobs(2, V, z[:3], None, 1, tokens, None, 1.0, n_top, **good, workspace=s.workspace)
+    assert all(torch.equal(good[k], kept[k]) for k in good)
