@@ -171,6 +171,7 @@ def bs_create(desc, weights, kv, workspace, B_max, k_max):
                          k_max, _stream(), C.byref(out))
     if st != BS_OK:
         raise BsError(st, "bs_create")
+    out.n_layers = desc.n_layers
     return out
 
 
@@ -379,6 +380,8 @@ def bs_kvq_bind(ctx, descs, workspace):
     if descs is None:
         _check(ctx, lib().bs_kvq_bind(ctx, None, None, 0))
         return
+    if len(descs) != ctx.n_layers:
+        raise BsError(BS_ESHAPE, "bs_kvq_bind: %d descriptions for %d layers" % (len(descs), ctx.n_layers))
     _check(ctx, lib().bs_kvq_bind(ctx, (bs_kvq_desc * len(descs))(*descs), _ptr(workspace), workspace.numel() * workspace.element_size()))
 
 

@@ -255,3 +255,14 @@ def test_steps_of_many_rows_and_long_contexts(shape, ctx, k_b, k_max, besides):
     eng.ctx_len[:n].copy_(H.dev_i32(ctx))
     slots = [int(s) for s in rng.permutation(n)]
     _step(eng, wn, H.oracle_desc(desc), slots, [ctx[s] for s in slots], [k_b[s] for s in slots], k_max, rng)
+
+
+def test_a_description_for_every_layer():
+    """The library reads as many descriptions as the model has layers: a shorter list is refused."""
+    desc = SHAPES["d128_g3"]
+    eng, _ = _engine(desc, 1, [100, 100], 3)
+    for descs in (eng.kvq.desc[:-1], eng.kvq.desc[:1], [], eng.kvq.desc + eng.kvq.desc[:1]):
+        with pytest.raises(B.BsError) as e:
+            B.bs_kvq_bind(eng.ctx, descs, eng._kvq_workspace)
+        assert e.value.status == B.BS_ESHAPE
+    B.bs_kvq_bind(eng.ctx, eng.kvq.desc, eng._kvq_workspace)
