@@ -324,7 +324,7 @@ bs_status bs_kvq_attention(const bs_kvq_desc* kv, int B, const int32_t* seq_slot
  * given pages of the 8-bit cache in their place: such a context makes its first step after this call, and from then on always has an 8-bit cache bound.  Rows
  * rejected by bs_kv_commit can leave a larger scale behind in their block until it is begun anew.
  * workspace (dev, 256-byte aligned, at least bs_kvq_bind_bytes, which is 0 for float32 models) is zero-filled once before the call and stays the
- * caller's; it must stay valid while bound.  layers == NULL unbinds (BS_ESTATE where bs_create was given pages of a cache that has been bound).  A pending
+ * caller's; it must stay valid while bound.  It can serve bs_kvq_attention calls of up to k_max + 1 rows, too, which must not overlap the steps in time.  layers == NULL unbinds (BS_ESTATE where bs_create was given pages of a cache that has been bound).  A pending
  * verify step is dropped; a call that fails leaves everything as it was.  Host call, no GPU work.
  * Errors: BS_EINVAL (null, float32 model, another block table, misaligned pointers), BS_ESHAPE (sizes differ from the context's, or B_max and k_max exceed what
  * bs_kvq_attention takes), BS_ECAPACITY (workspace too small, out of host memory). */

@@ -816,13 +816,13 @@ bs_status bs_kvq_attention(const bs_kvq_desc* kv, int B, const int32_t* seq_slot
 }
 
 namespace {
-// Staging pages of a step's K and V rows, then the attention workspace.
+// The attention workspace, then staging pages of a step's K and V rows.
 size_t kvq_bind_carve(const bs_ctx* c, char* base, void** k, void** v, void** ws) {
   Carver w{base};
   const size_t pages = (c->M_max + kPage - 1) / kPage * kv_page_elems(c->s.Hkv, c->s.D);
+  *ws = w.take<char>(kvq_attention_workspace(c->s.Hq, c->s.Hkv, c->s.D, c->k_max + 1));
   *k = w.take<uint16_t>(pages);
   *v = w.take<uint16_t>(pages);
-  *ws = w.take<char>(kvq_attention_workspace(c->s.Hq, c->s.Hkv, c->s.D, c->k_max + 1));
   return (w.off + 255) & ~(size_t)255;
 }
 }  // namespace

@@ -70,7 +70,7 @@ class Engine:
         self.kvq = None
         if kv_bits == 8:
             self.kvq = KvqCache(desc["n_layers"], desc["n_q_heads"], desc["n_kv_heads"], desc["head_dim"], n_slots, max_ctx, k_max + 1,
-                                device=self.device, block_table=self.block_table, n_pages=self.n_pages)
+                                device=self.device, block_table=self.block_table, n_pages=self.n_pages, own_workspace=False)
             self.k_pages, self.v_pages = self.kvq.k_pages, self.kvq.v_pages
         else:
             # pages are zero-initialised: masked positions still enter the P*V product with weight 0
@@ -89,6 +89,7 @@ class Engine:
         if self.kvq is not None:
             self._kvq_workspace = torch.zeros(max(B.bs_kvq_bind_bytes(self.ctx), 1), dtype=torch.uint8, device=self.device)
             B.bs_kvq_bind(self.ctx, self.kvq.desc, self._kvq_workspace)
+            self.kvq.workspace = self._kvq_workspace
         self._pool = None
 
     def close(self):
@@ -187,11 +188,12 @@ class Engine:
 class KvqCache:
     """Owns a KV cache in 8 bits (pages, scales and block table of every layer, attention workspace) and forwards to bs_kvq_*.
     Slots, capacities and page permutation as in Engine.  Rows are packed in batch order; n_max / q_max bound the rows of a
-    sequence, which are on the device.  One attention call at a time: the workspace is shared.  `status` (one int32 on the device) collects BS_FAULT_* bits until poll_status."""
+    sequence, which are on the device.  One attention call at a time: the workspace is shared (that of an Engine's cache with its verify
+    steps).  `status` (one int32 on the device) collects BS_FAULT_* bits until poll_status."""
 
     def __init__(self, n_layers, n_q_heads, n_kv_heads, head_dim, n_slots, max_ctx, q_max, device="cuda:0", page_perm_seed=None,
-                 slot_tokens=None, block_table=None, n_pages=0):
-        """block_table, n_pages: those of another owner (an Engine) instead of own ones."""
+                 slot_tokens=None, block_table=None, n_pages=0, own_workspace=True):
+        """block_table, n_pages: those of another owner (an Engine) instead of own ones, which sets `workspace` where own_workspace is False."""
         self.device = torch.device(device)
         self.n_q_heads, self.n_kv_heads, self.head_dim, self.n_slots, self.q_max = n_q_heads, n_kv_heads, head_dim, n_slots, q_max
         self.block_table, self.n_pages = (block_table, n_pages) if block_table is not None else page_table(n_slots, max_ctx, slot_tokens, page_perm_seed, self.device)
@@ -206,7 +208,7 @@ class KvqCache:
         nbytes = B.bs_kvq_workspace_bytes(n_q_heads, n_kv_heads, head_dim, q_max)
         if nbytes == 0:
             raise B.BsError(B.BS_ESHAPE, "bs_kvq_workspace_bytes rejected the shape")
-        self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+        self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device) if own_workspace else None
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
 
     def write(self, layer, seq_slot, pos0, n_rows, n_max, k_rows, v_rows):

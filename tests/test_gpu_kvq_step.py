@@ -13,6 +13,7 @@ from paper_2605_08862_amd import binding as B
 from paper_2605_08862_amd import workloads as W
 from paper_2605_08862_amd.runtime import Engine, KvqCache, LogprobScorer, fuse_weights
 from tests import helpers as H
+from tests.test_gpu_kvq import _close
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -266,3 +267,36 @@ def test_a_description_for_every_layer():
             B.bs_kvq_bind(eng.ctx, descs, eng._kvq_workspace)
         assert e.value.status == B.BS_ESHAPE
     B.bs_kvq_bind(eng.ctx, eng.kvq.desc, eng._kvq_workspace)
+
+
+@pytest.mark.parametrize("shape,k_max", [("d128_g3", 4), ("d128_g7", 16)])
+def test_attention_beside_steps_on_the_same_workspace(shape, k_max):
+    """Engine(kv_bits=8) holds one attention workspace, which its steps and calls of its cache take in turn."""
+    desc = SHAPES[shape]
+    rng = np.random.default_rng(k_max)
+    before = torch.cuda.memory_allocated()
+    cache = KvqCache(desc["n_layers"], desc["n_q_heads"], desc["n_kv_heads"], desc["head_dim"], 2, 9200, k_max + 1, device=DEV)
+    alone, nbytes = torch.cuda.memory_allocated() - before, cache.workspace.numel()
+    before = torch.cuda.memory_allocated()
+    beside = KvqCache(desc["n_layers"], desc["n_q_heads"], desc["n_kv_heads"], desc["head_dim"], 2, 9200, k_max + 1, device=DEV, own_workspace=False)
+    assert torch.cuda.memory_allocated() - before <= alone - nbytes and beside.workspace is None
+    eng, wn = _engine(desc, 5, [9200, 300], k_max)
+    assert eng.kvq.workspace.data_ptr() == eng._kvq_workspace.data_ptr()
+    ctx, k_b = [9000, 40], [k_max, 2]
+    for b in range(2):
+        for l, (k, v) in enumerate(W.context_kv(desc, ctx[b], 40 + b)):
+            eng.kv_write(l, b, 0, k.to(DEV), v.to(DEV))
+    eng.ctx_len.copy_(H.dev_i32(ctx))
+    args = (H.dev_i32([0, 1]), H.dev_i32([3, 4]), H.dev_i32(rng.integers(0, desc["vocab"], (2, k_max))), H.dev_i32(k_b), k_max)
+    want = eng.verify_step(*args, want_logits=True)
+    rows = [k_max + 1, 3]
+    q = torch.from_numpy(rng.normal(0, 1, (sum(rows), desc["n_q_heads"], desc["head_dim"]))).to(torch.bfloat16)
+    for _ in range(2):
+        out = eng.kvq.attention(1, q.to(DEV), H.dev_i32([0, 1]), H.dev_i32(ctx), H.dev_i32(rows), k_max + 1)
+        assert torch.equal(eng.verify_step(*args, want_logits=True), want)
+        at = 0
+        for b in range(2):
+            k, v = (t.double().cpu().numpy() for t in eng.kv_read(1, b, 0, ctx[b] + rows[b]))
+            _close(out[at:at + rows[b]], q[at:at + rows[b]], k, v, ctx[b])
+            at += rows[b]
+    assert eng.poll_status() == 0 and eng.kvq.poll_status() == 0
