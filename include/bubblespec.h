@@ -276,10 +276,10 @@ bs_status bs_kv_read(bs_ctx* ctx, int layer, int slot, int pos0, int n, void* k_
  * These calls need no context.  The caller owns all memory.  They only enqueue work on `stream` (of the current device), can be
  * captured into a HIP graph, and report conditions only the device can see in `status` (dev, one int32 word that the caller
  * clears; BS_FAULT_* bits are or-ed into it; may be NULL).  Rows are packed in batch order: sequence b has n[b] rows, which start
- * at sum_{b'<b} n[b'] (a count outside [0, n_max] sets BS_FAULT_DRAFT_LEN and counts as 0).  A sequence with a bad slot
- * (BS_FAULT_SLOT), or with positions or page ids outside the cache (BS_FAULT_KV_PAGES), is skipped: its rows of the outputs and
- * its pages stay as they are.  (Attention, a bad page id: the rows that see it stay as they are; those before them may, too.)  A sequence without rows is
- * skipped whatever its slot is (padded batches). */
+ * at sum_{b'<b} n[b'] (a count outside [0, n_max] sets BS_FAULT_DRAFT_LEN and counts as 0); the caller's rows are no fewer than the
+ * counts add up to.  A sequence with a bad slot (BS_FAULT_SLOT), or with positions or page ids outside the cache
+ * (BS_FAULT_KV_PAGES), is skipped: its rows of the outputs and its pages stay as they are.  (Attention, a bad page id: the rows that
+ * see it stay as they are; those before them may, too.)  A sequence without rows is skipped whatever its slot is (padded batches). */
 typedef struct {
   int32_t n_pages, n_slots, max_pages_per_seq, n_kv_heads, head_dim;
   void* k_pages;              /* dev [n_pages] pages of n_kv_heads * BS_PAGE_TOKENS * head_dim bytes, 16-byte aligned; element  */
@@ -324,8 +324,9 @@ bs_status bs_kvq_attention(const bs_kvq_desc* kv, int B, const int32_t* seq_slot
  * given pages of the 8-bit cache in their place: such a context makes its first step after this call, and from then on always has an 8-bit cache bound.  Rows
  * rejected by bs_kv_commit can leave a larger scale behind in their block until it is begun anew.
  * workspace (dev, 256-byte aligned, at least bs_kvq_bind_bytes, which is 0 for float32 models) is zero-filled once before the call and stays the
- * caller's; it must stay valid while bound.  It can serve bs_kvq_attention calls of up to k_max + 1 rows, too, which must not overlap the steps in time.  layers == NULL unbinds (BS_ESTATE where bs_create was given pages of a cache that has been bound).  A pending
- * verify step is dropped; a call that fails leaves everything as it was.  Host call, no GPU work.
+ * caller's; it must stay valid while bound.  It can serve bs_kvq_attention calls of up to k_max + 1 rows, too, which must not overlap the steps in time.
+ * layers == NULL unbinds (BS_ESTATE where bs_create was given pages of a cache that has been bound).  A pending verify step is dropped; a call that fails leaves
+ * everything as it was.  Host call, no GPU work.
  * Errors: BS_EINVAL (null, float32 model, another block table, misaligned pointers), BS_ESHAPE (sizes differ from the context's, or B_max and k_max exceed what
  * bs_kvq_attention takes), BS_ECAPACITY (workspace too small, out of host memory). */
 size_t bs_kvq_bind_bytes(const bs_ctx* ctx);
@@ -333,7 +334,10 @@ bs_status bs_kvq_bind(bs_ctx* ctx, const bs_kvq_desc* layers /*host[L] or NULL*/
 
 /* ---------------------------------------------------------------------------------------------
  * Log probabilities of a rollout's tokens under the distribution that made them (what importance weights need when rollouts come
- * from a quantised cache or an older policy), the entropy of that distribution and its best alternatives.
+ * from a quantised cache or an older policy), the entropy of that distribution and its best alternatives.  That distribution is the softmax of the logits
+ * passed: the one that accept calls sample from at a temperature above 0 with no filter.  With a filter (bs_set_filter) they sample from a truncated,
+ * renormalised law, which these logits do not say: the caller masks the tokens that it dropped (-inf), or has the values of the unfiltered law.  At
+ * temperature 0, refused here, an emitted token is the arg-max with probability 1.
  * logits [M, vocab] (dev, logits_dtype, dense) are packed as in bs_accept_resample_logits: sequence b has draft_len[b] + 1 rows
  * (draft_len == NULL: k_max + 1 each); token i < n_tokens[b] <= draft_len[b] + 1 (NULL: all rows) of sequence b is tokens[b][i], judged by row i.
  * So the outputs of an accept call can be passed on: tokens = out_tokens, n_tokens = n_emitted.  Over p = softmax(logits / temperature):

@@ -239,7 +239,8 @@ class KvqCache:
 
 class LogprobScorer:
     """Owns the workspace of bs_token_logprobs for up to B_max sequences of k_max + 1 rows.  The tokens, counts and logits of an
-    accept call can be passed on; `status` collects BS_FAULT_* bits until poll_status.  One call at a time: the workspace is shared."""
+    accept call can be passed on; `status` collects BS_FAULT_* bits until poll_status.  One call at a time: the workspace is shared.  The law is the softmax of
+    the logits passed: for tokens sampled under Engine.set_filter the caller masks (-inf) what the filter dropped, else log p is that of the unfiltered law."""
 
     def __init__(self, B_max, k_max, vocab, n_top, device="cuda:0"):
         self.B_max, self.k_max, self.vocab, self.n_top = B_max, k_max, vocab, n_top

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import accept as OA
 from oracle import logprobs as O
 from paper_2605_08862_amd import binding as B
 from paper_2605_08862_amd.runtime import LogprobScorer
@@ -218,3 +219,24 @@ def test_outputs_of_another_type_or_too_short_are_refused():
     with pytest.raises(B.BsError):
         B.bs_token_logprobs(2, V, z[:3], None, 1, tokens, None, 1.0, n_top, **good, workspace=s.workspace)
     assert all(torch.equal(good[k], kept[k]) for k in good)
+
+
+@pytest.mark.parametrize("top_k,top_p", [(5, 1.0), (0, 0.7), (40, 0.9)])
+def test_the_law_of_a_filtered_sampler_from_masked_logits(top_k, top_p):
+    """Rows as they are give log p under the unfiltered law; with the tokens masked that the filter drops, under the law that was sampled from.  |y| < 2^5 here: y and
+    the logarithm are off by less than 2^-18 in all."""
+    V, T, n_top = 3000, 0.8, 6
+    z = torch.from_numpy(np.random.default_rng(top_k + 1).normal(0, 3.0, (4, V)).astype(np.float32))
+    masked, tokens = torch.full_like(z, -INF), np.zeros((4, 1), dtype=np.int64)
+    for i in range(4):
+        keep, _ = OA.kept_tokens(z[i].numpy(), T, top_k, top_p)
+        masked[i, keep] = z[i, keep]
+        tokens[i] = keep[-1]
+    s = LogprobScorer(4, 0, V, n_top, device=DEV)
+    raw, out = s(z.to(DEV), _i32(tokens), temperature=T), s(masked.to(DEV), _i32(tokens), temperature=T)
+    _check(raw, z, tokens, [1] * 4, [0] * 4, T, n_top)
+    _check(out, masked, tokens, [1] * 4, [0] * 4, T, n_top)
+    for i in range(4):
+        p = OA.filtered_probs(z[i].double().numpy(), T, top_k, top_p)
+        assert abs(float(out["logprob"][i, 0]) - np.log(p[tokens[i, 0]])) < 2.0 ** -17 and abs(float(out["entropy"][i, 0]) + (p[p > 0] * np.log(p[p > 0])).sum()) < 2.0 ** -17
+        assert float(raw["logprob"][i, 0]) < float(out["logprob"][i, 0])
