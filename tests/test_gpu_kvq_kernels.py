@@ -85,3 +85,23 @@ def test_rows_beside_a_bad_page(Hq, Hkv, D, ctx, counts, page, besides):
         left = (out == 3.0).all(-1, keepdim=True)
         assert not bool(left[:first].any())
         _close_on_gpu(x, torch.where(left, clean, out), q, slots, ctx, counts[:b] + [seen])
+
+
+@pytest.mark.parametrize("wide", [False, True], ids=["few", "many"])
+@pytest.mark.parametrize("k_size,v_size", [(2.0 ** -19, 2.0 ** -20), (1.0, 2.0 ** -17), (4000.0, 9000.0), (2.0 ** -6, 3.0)])
+def test_smallest_and_largest_scales(k_size, v_size, wide):
+    """Values that are subnormal in float16 (multiples of 2^-24), and scores of many thousands."""
+    Hq, Hkv, D, ctx, counts = 28, 4, 128, [100, 0, 64, 257, 31, 5, 90, 200, 12], [9, 3, 1, 9, 2, 9, 9, 9, 9]
+    rng = np.random.default_rng(17)
+    held = [c + r for c, r in zip(ctx, counts)]
+    n = len(ctx)
+    cache = KvqCache(1, Hq, Hkv, D, n + 1, 0, max(counts), device=DEV, slot_tokens=held + [40000 if wide else 1])
+    x = Both.__new__(Both)
+    x.dims, x.caps, x.cache = (Hq, Hkv, D), held, cache
+    k, v = (torch.from_numpy(rng.normal(0, s, (sum(held), Hkv, D))).to(torch.bfloat16).to(DEV) for s in (k_size, v_size))
+    slots = list(range(n))
+    cache.write(0, _i32(slots), _i32([0] * n), _i32(held), max(held), k, v)
+    q = torch.from_numpy(rng.normal(0, 1.0, (sum(counts), Hq, D))).to(torch.bfloat16).to(DEV)
+    out = cache.attention(0, q, _i32(slots), _i32(ctx), _i32(counts), max(counts))
+    _close_on_gpu(x, out, q, slots, ctx, counts)
+    assert cache.poll_status() == 0
