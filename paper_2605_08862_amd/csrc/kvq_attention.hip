@@ -354,8 +354,8 @@ template <bool STEP> __device__ __forceinline__ u32x4 query8(u32x4 v, bool& rang
 
 // Blocks of up to 32 rows, four waves, two workgroups on a CU.  STEP: inside bs_verify_step (float16 queries, output in chunk order).  Every wave has two tiles of K
 // and V codes in registers and loads the next but one behind the products that read them.
-// What bounds it: memory, where there are steps enough (7B heads, 64 sequences of 4096 tokens, one row: 57 us, 4.7 TB/s); else the way to the first tile and the
-// merges (1.5B heads, one row of 30001 tokens: 15.5 us).
+// What bounds it: memory, where there are steps enough (7B heads, 64 sequences of 4096 tokens, one row: 56 us, 4.8 TB/s); else the way to the first tile and the
+// merges (1.5B heads, one row of 30001 tokens: 14.9 us).
 template <int D, bool STEP>
 __global__ void __launch_bounds__(256, 2) kvq_attention_kernel(BS_KVQ_PARAMS) {
   constexpr int KS = D / 16, DT = D / 32, RP = 32, CH = D / 4;
@@ -519,7 +519,7 @@ __device__ __forceinline__ void copy_to_lds(const uint8_t* src, char* dst) {
 // the memory pipeline copies it there (global -> LDS loads, a share of the 1 KiB pieces by each wave), NB buffers for each phase, NB - 1 tiles in flight and one
 // barrier per tile.
 // What bounds it: two query tiles, memory; four, that matrix and vector instructions of the two waves of a SIMD overlap in part only.  7B heads, 32 sequences of 8192
-// tokens (memory 57 us), 9 rows 65 us, 17 rows 98 .. 103.  Of the latter, at 105 then, with parts left out: the way to the first tile and the merges 22, copying the tiles
+// tokens (memory 57 us), 9 rows 64 .. 68 us, 17 rows 98 .. 103.  Of the latter, at 105 then, with parts left out: the way to the first tile and the merges 22, copying the tiles
 // alone 69, matrix instructions alone 84 (half of their nominal rate, as a large matrix product has it too), everything but them 87, everything but the softmax 90,
 // everything but the conversions 100.  Two tiles per barrier, a tile of K read ahead, requests behind the scores: the same or slower; twelve waves with three phases:
 // 12 us more; scores of the next tile multiplied while this one's become probabilities: 10 us more; the two waves of a SIMD held half a tile apart by barriers: 10 us more;

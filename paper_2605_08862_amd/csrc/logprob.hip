@@ -6,7 +6,8 @@
 // One pass over the logits, bound by memory.  A row is cut into segments, a workgroup each, which keeps its segment in registers: every wave sums against its own
 // maximum, and the best alternatives come from a bound.  The largest of 64 groups of threads are known from the maxima; the n-th largest of these is no larger
 // than the n-th largest logit, and hardly any other logit reaches it, so that one comparison per logit leaves a short list (a few more than n), which is ranked by
-// counting.  The last segment of a row to arrive (publish_arrival, common.h) merges maxima, sums and lists the same way.
+// counting.  Where more than kList of a segment reach it (logits that are all alike, or within 2^-7 of each other), the alternatives are looked for one after the
+// other in n passes over the segment: 1152 rows of 152064 such float32 words 4350 us, bf16 3270, instead of 142 and 104.  The last segment of a row to arrive (publish_arrival, common.h) merges maxima, sums and lists the same way.
 #include "logprob.h"
 
 namespace {

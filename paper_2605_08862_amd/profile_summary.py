@@ -23,6 +23,8 @@ A case of perf/cases.py (C = its name) instead of a bench.py workload, kernel tr
 the main phase there too (a sampler case clears the status word in every call):
   PYTHONPATH=<checkout> rocprofv3 --kernel-trace --stats -d OUT/kt -o kt -- python3 -c "<CASE_DRIVER>" C
   python3 -m paper_2605_08862_amd.profile_summary --case C --kt OUT/kt >> profiles/cases_kernels.txt
+
+A case of perf/operators.py the same way, with <OPERATOR_DRIVER> and --operator C; the calls that fill its cache are counted with the passes.
 """
 import argparse
 import glob
@@ -34,6 +36,8 @@ import sys
 CLASS_ORDER = ["attention", "gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down", "lmhead"]
 CASE_DRIVER = ("import sys, torch; from perf import cases as C; s = C.prepare([c for c in C.listed() if c['name'] == sys.argv[1]][0], 1); "
                "[C.run(s) for _ in range(5)]; 'eng' in s and s['eng'].poll_status(); [C.run(s) for _ in range(30)]; torch.cuda.synchronize()")
+OPERATOR_DRIVER = ("import sys, torch; from perf import operators as O; O.own = True; s = O.prepare([c for c in O.listed() if c['name'] == sys.argv[1]][0], 1); "
+                   "[O.run(s) for _ in range(35)]; torch.cuda.synchronize()")
 CALIBRATION_KIB = 262144.0          # the 256 MiB copy of bench.py --copy-calibration
 
 
@@ -193,6 +197,7 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--workload")
     ap.add_argument("--case", help="a case of perf/cases.py was run instead of a bench.py workload")
+    ap.add_argument("--operator", help="a case of perf/operators.py was run instead of a bench.py workload")
     ap.add_argument("--kt", help="directory of the --kernel-trace run")
     ap.add_argument("--fetch", help="directory of the --pmc FETCH_SIZE run (with --copy-calibration)")
     ap.add_argument("--write", help="directory of the --pmc WRITE_SIZE run (with --copy-calibration)")
@@ -201,8 +206,9 @@ def main():
     ap.add_argument("--bench-args", default="", help="further bench.py arguments every pass was run with (e.g. '--layers 2')")
     ap.add_argument("--note", action="append", default=[], help="free text for the header (repeatable)")
     args = ap.parse_args()
-    if args.case:
-        lines = ["rocprofv3 --kernel-trace --stats -d OUT/kt -o kt -- python3 -c \"<CASE_DRIVER of profile_summary.py>\" %s   (one MI355X)" % args.case]
+    if args.case or args.operator:
+        lines = ["rocprofv3 --kernel-trace --stats -d OUT/kt -o kt -- python3 -c \"<%s_DRIVER of profile_summary.py>\" %s   (one MI355X)"
+                 % ("CASE" if args.case else "OPERATOR", args.case or args.operator)]
         kernel_trace(args.kt, lines)
         print("\n".join(lines) + "\n")
         return
