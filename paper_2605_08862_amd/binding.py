@@ -380,8 +380,9 @@ def bs_kvq_bind(ctx, descs, workspace):
     if descs is None:
         _check(ctx, lib().bs_kvq_bind(ctx, None, None, 0))
         return
-    if len(descs) != ctx.n_layers:
-        raise BsError(BS_ESHAPE, "bs_kvq_bind: %d descriptions for %d layers" % (len(descs), ctx.n_layers))
+    n_layers = getattr(ctx, "n_layers", len(descs))                        # (of a handle that bs_create above has made)
+    if len(descs) != n_layers:
+        raise BsError(BS_ESHAPE, "bs_kvq_bind: %d descriptions for %d layers" % (len(descs), n_layers))
     _check(ctx, lib().bs_kvq_bind(ctx, (bs_kvq_desc * len(descs))(*descs), _ptr(workspace), workspace.numel() * workspace.element_size()))
 
 

@@ -226,6 +226,8 @@ class KvqCache:
         """q: bf16 [rows, n_q_heads, head_dim]; row i of sequence b sees positions 0 .. ctx_len[b] + i."""
         if q_max > self.q_max:
             raise B.BsError(B.BS_ECAPACITY, "KvqCache.attention: q_max exceeds that of the workspace")
+        if self.workspace is None:
+            raise B.BsError(B.BS_ESTATE, "KvqCache.attention: the cache was made without a workspace, and none has been set")
         if out is None:
             out = torch.empty(q.shape[0], self.n_q_heads, self.head_dim, dtype=torch.bfloat16, device=self.device)
         B.bs_kvq_attention(self.desc[layer], seq_slot.numel(), seq_slot, ctx_len, q_len, q_max, self.n_q_heads, q, out, self.workspace, self.status)

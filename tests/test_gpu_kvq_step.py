@@ -280,6 +280,9 @@ def test_attention_beside_steps_on_the_same_workspace(shape, k_max):
     before = torch.cuda.memory_allocated()
     beside = KvqCache(desc["n_layers"], desc["n_q_heads"], desc["n_kv_heads"], desc["head_dim"], 2, 9200, k_max + 1, device=DEV, own_workspace=False)
     assert torch.cuda.memory_allocated() - before <= alone - nbytes and beside.workspace is None
+    with pytest.raises(B.BsError) as e:
+        beside.attention(0, torch.zeros(1, desc["n_q_heads"], desc["head_dim"], dtype=torch.bfloat16, device=DEV), H.dev_i32([0]), H.dev_i32([0]), H.dev_i32([1]), 1)
+    assert e.value.status == B.BS_ESTATE
     eng, wn = _engine(desc, 5, [9200, 300], k_max)
     assert eng.kvq.workspace.data_ptr() == eng._kvq_workspace.data_ptr()
     ctx, k_b = [9000, 40], [k_max, 2]
